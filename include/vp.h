@@ -63,8 +63,10 @@ typedef enum {
 enum {
     VP_SAVE_LOGITS = 1u, /* fwd: store the logits; bwd: the stored logits are supplied */
     VP_SKIP_DH = 2u,     /* vp_output_bwd only: pass T of Algorithm 2, dW_shard alone (dH_accum may be NULL) */
-    VP_DH_OVERWRITE = 4u /* vp_output_bwd, vp_output_dx_alg2: dH_accum = (this shard's term) instead of +=: the first
-                            term of the reduce C2, which saves zero-filling dH_accum and reading the zeros back */
+    VP_DH_OVERWRITE = 4u, /* vp_output_bwd, vp_output_dx_alg2: dH_accum = (this shard's term) instead of +=: the first
+                             term of the reduce C2, which saves zero-filling dH_accum and reading the zeros back */
+    VP_NORM_POST = 8u,    /* vp_block_norm_*: the block's output is normalised before it joins the residual stream */
+    VP_NORM_CENTER = 16u  /* vp_block_norm_*: norms subtract the mean of the row (layer norm; without it RMS norm) */
 };
 
 /* Library version (major*10000 + minor*100 + patch). Host-only, no device work. */
@@ -290,6 +292,81 @@ vp_status vp_embed_fwd_group(const void* const* table_shards, const int64_t* ids
 vp_status vp_embed_bwd_group(const void* grad_out, const int64_t* ids, int32_t p, int64_t N, int64_t h, int64_t Vs,
                              int64_t shard_offset, vp_dtype dt, float* const* dtable_shards, void* workspace,
                              size_t workspace_bytes, void* stream);
+
+/*
+ * The norms around a block of the model: what comes between the last block and the output layer (H is what vp_output_fwd
+ * reads), and between any two blocks.  x is the residual stream, y what the block made of it.  With the mean m of a row
+ * (0 without VP_NORM_CENTER) and rho = 1 / sqrt(mean_j (v_j - m)^2 + eps), for every token i
+ *     u_i = (y_i - m1_i) rho1_i w_post + b_post      with VP_NORM_POST (m1, rho1 of y_i), else u_i = y_i
+ *     r_i = x_i + scale * gate_k u_i                 k = floor(i gate_rows / N)
+ *     H_i = (r_i - m2_i) rho2_i w + b                (m2, rho2 of r_i before it is rounded to type dt)
+ * all in fp32, rounded once to type dt.  y == NULL: r = x, the norm alone (r, gate, w_post and b_post are then NULL).
+ *   x, y [N,h] : in, type dt.  gate [gate_rows,h] : in, type dt, or NULL with gate_rows = 0 (no gate).  gate_rows divides N:
+ *   1 is a gate per channel, N an element-wise one, anything between one per sequence of N / gate_rows tokens.
+ *   w_post, b_post, w, b [h] : in, type dt, or NULL (1 and 0).
+ *   r [N,h] : out, type dt, or NULL (not kept).  H [N,h] : out, type dt.
+ *   stats [4,N] : out, fp32, or NULL: m1, rho1 (0 and 1 without VP_NORM_POST), m2, rho2, which the backward call reads.
+ * r may be x and H may be y (in place); apart from that no output shares memory with an input or another output.
+ * Squares are summed in fp32: rows whose sum of squares exceeds 3.4e38 give rho = 0.
+ * eps > 0.  Sizes as above, and h <= 2^20, N h < 2^31.
+ */
+vp_status vp_block_norm_fwd(const void* x, const void* y, const void* gate, int64_t gate_rows, const void* w_post,
+                            const void* b_post, const void* w, const void* b, int64_t N, int64_t h, vp_dtype dt,
+                            uint32_t flags, float scale, float eps, void* r, void* H, float* stats, void* stream);
+
+/*
+ * The gradients of vp_block_norm_fwd.  dH is the gradient of H, dr what else reaches r (the residual stream behind it; NULL:
+ * nothing).  With rh = (r - m2) rho2, a = dH w, yh = (y - m1) rho1 and means over the row
+ *     dx = dr + rho2 (a - mean(a) - rh mean(a rh))             (mean(a) with VP_NORM_CENTER alone)
+ *     d  = scale * gate_k dx
+ *     dy = rho1 (c - mean(c) - yh mean(c yh)), c = d w_post    with VP_NORM_POST, else dy = d
+ *     dw = sum_i dH rh,  db = sum_i dH,  dw_post = sum_i d yh,  db_post = sum_i d       (over the tokens)
+ *     dgate_k = sum over the tokens of row k of  scale * u dx,  u = yh w_post + b_post
+ * Sums run in a fixed order: results repeat bit for bit.
+ *   dH [N,h] : in, type dH_dt (vp_output_bwd leaves fp32).  dr [N,h] : in, type grad_dt.
+ *   r [N,h] : in, type dt, as the forward call wrote it (x where y was NULL).  y, gate, w_post, b_post, w, stats, scale, flags:
+ *   as given to and left by the forward call (y == NULL: the norm alone; dy and the gradients of gate and post norm are NULL).
+ *   dx, dy [N,h] : out, type grad_dt.  dgate [gate_rows,h], dw_post, db_post, dw, db [h] : out, fp32, overwritten; each may
+ *   be NULL (not wanted).
+ * With dt = VP_F32, dH_dt and grad_dt are VP_F32 too.  dx may be dr; apart from that no output shares memory with an input or
+ * another output.  The workspace has vp_block_norm_bwd_workspace_bytes(...) bytes ((size_t)-1 for invalid arguments).
+ */
+size_t vp_block_norm_bwd_workspace_bytes(int64_t N, int64_t h, int64_t gate_rows, uint32_t flags);
+vp_status vp_block_norm_bwd(const void* dH, vp_dtype dH_dt, const void* dr, const void* r, const void* y, const void* gate,
+                            int64_t gate_rows, const void* w_post, const void* b_post, const void* w, const float* stats,
+                            int64_t N, int64_t h, vp_dtype dt, uint32_t flags, float scale, vp_dtype grad_dt, void* dx,
+                            void* dy, float* dgate, float* dw_post, float* db_post, float* dw, float* db, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/*
+ * The norm of all gradients of a step together, and clipping by it.  grads is a HOST array of n device pointers, counts and
+ * dts HOST arrays of their numbers of elements (0: the pointer may be NULL) and types; all are read before the call returns.
+ * Gradients may start at any element (4 bytes with VP_F32, 2 with VP_BF16).
+ *     norm[0] = sqrt( sum over all elements of all gradients of g^2 )
+ * Squares are formed and summed in fp64, in a fixed order: none over- or underflows, results repeat bit for bit.
+ *   norm [1] : out, fp32.  The workspace has vp_grad_workspace_bytes(n) bytes ((size_t)-1 for n < 0).
+ */
+size_t vp_grad_workspace_bytes(int32_t n);
+vp_status vp_grad_norm(const void* const* grads, const int64_t* counts, const int32_t* dts, int32_t n, float* norm,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * vp_grad_norm, and the gradients clipped by it:
+ *     outs[k] = grads[k] * f,   f = norm > max_norm and norm finite ? max_norm / norm : 1
+ * in fp32, rounded once.  outs is a HOST array of n device pointers to tensors of the gradients' sizes and types, or NULL (in
+ * place: nothing is written where f = 1).  An output may be the gradient of the same index and shares no memory with anything
+ * else.  A norm that is not finite leaves the gradients as they are: the caller sees it in norm and leaves the step out.
+ * max_norm >= 0 and finite.
+ */
+vp_status vp_grad_clip(const void* const* grads, const int64_t* counts, const int32_t* dts, int32_t n, void* const* outs,
+                       float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The second half of vp_grad_clip alone, with a norm that is known already (such as one summed over several devices):
+ * norm [1] is in.
+ */
+vp_status vp_grad_scale(const void* const* grads, const int64_t* counts, const int32_t* dts, int32_t n, void* const* outs,
+                        float max_norm, const float* norm, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Measurement aid, not part of the method.  While enabled, every kernel launch made by the

@@ -9,6 +9,7 @@ twice as long).  The library has no fallback: if it is missing or a call fails, 
 """
 from __future__ import annotations
 
+import bisect
 import ctypes
 import importlib.util
 import os
@@ -22,6 +23,8 @@ VP_BF16 = 1
 VP_SAVE_LOGITS = 1
 VP_SKIP_DH = 2
 VP_DH_OVERWRITE = 4
+VP_NORM_POST = 8
+VP_NORM_CENTER = 16
 
 VP_CALL_OUTPUT_FWD = 0
 VP_CALL_COMBINE_STATS = 1
@@ -120,6 +123,21 @@ def load_library() -> ctypes.CDLL:
     lib.vp_embed_fwd_group.argtypes = [vp, vp, i32, i64, i64, i64, i64, c.c_int, vp, vp]
     lib.vp_embed_bwd_group.restype = c.c_int
     lib.vp_embed_bwd_group.argtypes = [vp, vp, i32, i64, i64, i64, i64, c.c_int, vp, vp, sz, vp]
+    lib.vp_block_norm_fwd.restype = c.c_int
+    lib.vp_block_norm_fwd.argtypes = [vp, vp, vp, i64, vp, vp, vp, vp, i64, i64, c.c_int, u32, fl, fl, vp, vp, vp, vp]
+    lib.vp_block_norm_bwd_workspace_bytes.restype = sz
+    lib.vp_block_norm_bwd_workspace_bytes.argtypes = [i64, i64, i64, u32]
+    lib.vp_block_norm_bwd.restype = c.c_int
+    lib.vp_block_norm_bwd.argtypes = [vp, c.c_int, vp, vp, vp, vp, i64, vp, vp, vp, vp, i64, i64, c.c_int, u32, fl, c.c_int,
+                                      vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.vp_grad_workspace_bytes.restype = sz
+    lib.vp_grad_workspace_bytes.argtypes = [i32]
+    lib.vp_grad_norm.restype = c.c_int
+    lib.vp_grad_norm.argtypes = [vp, vp, vp, i32, vp, vp, sz, vp]
+    lib.vp_grad_clip.restype = c.c_int
+    lib.vp_grad_clip.argtypes = [vp, vp, vp, i32, vp, fl, vp, vp, sz, vp]
+    lib.vp_grad_scale.restype = c.c_int
+    lib.vp_grad_scale.argtypes = [vp, vp, vp, i32, vp, fl, vp, vp, sz, vp]
     lib.vp_profile_mfma_loop.restype = c.c_int
     lib.vp_profile_mfma_loop.argtypes = [vp, vp, i32, i32, vp]
     lib.vp_profile_mfma_variant.restype = c.c_int
@@ -513,6 +531,158 @@ def vp_embed_bwd_group(grad_out, ids, shard_offset: int, dtable_shards, workspac
         _ptr(grad_out, "grad_out"), _ptr(ids, "ids", (torch.int64,), (N,)), len(dtable_shards), N, h, Vs, shard_offset,
         _dtype_code(grad_out), _ptrs(dtable_shards, "dtable_shards", (torch.float32,), (Vs, h)), wp, wb, _stream(stream))
     _check(st, "vp_embed_bwd_group")
+
+
+def _on_current_device(ts) -> None:
+    """Refuses tensors of another device than the current one, whose stream the call would go to."""
+    if _HOST is not None and _HOST.on_current_device(ts):
+        return
+    here = torch.cuda.current_device()
+    for t in ts:
+        if t is not None and t.is_cuda and t.get_device() != here:
+            raise VPError("tensor on %s, but the current device is cuda:%d" % (t.device, here))
+
+
+def _norm_flags(post: bool, center: bool) -> int:
+    return (VP_NORM_POST if post else 0) | (VP_NORM_CENTER if center else 0)
+
+
+def _gate_rows(gate) -> int:
+    if gate is None:
+        return 0
+    if gate.dim() != 2:
+        raise VPError("gate must be [rows, h]")
+    return gate.shape[0]
+
+
+def vp_block_norm_fwd(x, y, H, *, r=None, stats=None, gate=None, w=None, b=None, w_post=None, b_post=None, scale: float = 1.0,
+                      eps: float = 1e-5, post: bool = False, center: bool = False, stream=None) -> None:
+    """The norms around a block: u = norm(y) (post) or y, r = x + scale * gate * u, H = norm(r); RMS norms, or layer norms with
+    center=True.  y=None: H = norm(x) alone.  r, stats ([4, N], for the backward call) and every vector may be None."""
+    if x.dim() != 2:
+        raise VPError("x must be [N, h]")
+    N, h = x.shape
+    dt = _dtype_code(x)
+    same = (torch.float32,) if dt == VP_F32 else _BF16_LIKE
+    rows = _gate_rows(gate)
+    _on_current_device((x, y, H, r, stats, gate, w, b, w_post, b_post))
+    st = load_library().vp_block_norm_fwd(
+        _ptr(x, "x"), _ptr(y, "y", same, (N, h)), _ptr(gate, "gate", same, (rows, h)), rows,
+        _ptr(w_post, "w_post", same, (h,)), _ptr(b_post, "b_post", same, (h,)), _ptr(w, "w", same, (h,)),
+        _ptr(b, "b", same, (h,)), N, h, dt, _norm_flags(post, center), scale, eps, _ptr(r, "r", same, (N, h)),
+        _ptr(H, "H", same, (N, h)), _ptr(stats, "stats", (torch.float32,), (4, N)), _stream(stream))
+    _check(st, "vp_block_norm_fwd")
+
+
+def vp_block_norm_bwd_workspace_bytes(N: int, h: int, gate_rows: int = 0, post: bool = False) -> int:
+    n = load_library().vp_block_norm_bwd_workspace_bytes(N, h, gate_rows, _norm_flags(post, False))
+    if n == ctypes.c_size_t(-1).value:
+        raise VPError("vp_block_norm_bwd_workspace_bytes: invalid arguments")
+    return n
+
+
+def vp_block_norm_bwd(dH, r, y, stats, *, dx, dy=None, dr=None, gate=None, w=None, w_post=None, b_post=None, scale: float = 1.0,
+                      post: bool = False, center: bool = False, dgate=None, dw=None, db=None, dw_post=None, db_post=None,
+                      workspace=None, stream=None) -> None:
+    """The gradients of vp_block_norm_fwd, from its r (x where y was None) and stats.  dH is fp32 or of the type of r; dr, dx
+    and dy are of one type, fp32 or that of r; the parameters' gradients are fp32, and None where they are not wanted."""
+    if r.dim() != 2:
+        raise VPError("r must be [N, h]")
+    N, h = r.shape
+    dt, dH_dt, grad_dt = _dtype_code(r), _dtype_code(dH), _dtype_code(dx)
+    f = (torch.float32,)
+    same = f if dt == VP_F32 else _BF16_LIKE
+    grad = f if grad_dt == VP_F32 else _BF16_LIKE
+    rows = _gate_rows(gate)
+    _on_current_device((dH, r, y, stats, dx, dy, dr, gate, w, w_post, b_post, dgate, dw, db, dw_post, db_post, workspace))
+    wp, wb = _ws(workspace)
+    st = load_library().vp_block_norm_bwd(
+        _ptr(dH, "dH", None, (N, h)), dH_dt, _ptr(dr, "dr", grad, (N, h)), _ptr(r, "r"), _ptr(y, "y", same, (N, h)),
+        _ptr(gate, "gate", same, (rows, h)), rows, _ptr(w_post, "w_post", same, (h,)), _ptr(b_post, "b_post", same, (h,)),
+        _ptr(w, "w", same, (h,)), _ptr(stats, "stats", f, (4, N)), N, h, dt, _norm_flags(post, center), scale, grad_dt,
+        _ptr(dx, "dx", grad, (N, h)), _ptr(dy, "dy", grad, (N, h)), _ptr(dgate, "dgate", f, (rows, h)),
+        _ptr(dw_post, "dw_post", f, (h,)), _ptr(db_post, "db_post", f, (h,)), _ptr(dw, "dw", f, (h,)), _ptr(db, "db", f, (h,)),
+        wp, wb, _stream(stream))
+    _check(st, "vp_block_norm_bwd")
+
+
+class GradientArguments:
+    """The host arrays that the calls over many gradients take.  It holds raw addresses: the tensors have to live, and to stay
+    where they are, as long as it is used (it keeps them alive).  outs: where the clipped gradients go, None = in place."""
+
+    def __init__(self, grads, outs=None):
+        self.grads, self.outs = list(grads), None if outs is None else list(outs)
+        n = self.n = len(self.grads)
+        if outs is not None and len(self.outs) != n:
+            raise VPError("outs: one tensor per gradient")
+        self.ptrs = (ctypes.c_void_p * n)(*[_ptr(g, "grads") for g in self.grads])
+        self.counts = (ctypes.c_int64 * n)(*[g.numel() for g in self.grads])
+        self.dts = (ctypes.c_int32 * n)(*[_dtype_code(g) for g in self.grads])
+        self.out_ptrs = None
+        if outs is not None:
+            self.out_ptrs = (ctypes.c_void_p * n)(*[_ptr(o, "outs", (g.dtype,), g.shape) for g, o in zip(self.grads, self.outs)])
+        self.devices = {t.get_device() for t in self.grads + (self.outs or [])}
+        # What is written is written by no order: outputs are apart from one another and from all gradients but their own.
+        written = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), k)
+                         for k, t in enumerate(self.grads if outs is None else self.outs) if t.numel())
+        self.overlap = any(a[1] > b[0] for a, b in zip(written, written[1:]))
+        if outs is not None and not self.overlap:
+            starts = [a[0] for a in written]
+            for k, g in enumerate(self.grads):
+                first, end = g.data_ptr(), g.data_ptr() + g.numel() * g.element_size()
+                at = bisect.bisect_right(starts, first) - 1
+                for a in written[max(at, 0):]:
+                    if a[0] >= end:
+                        break
+                    if a[1] > first and first < end and not (a[2] == k and a[0] == first):
+                        self.overlap = True
+
+
+def _grad_call(name: str, a, written: bool, call, norm, workspace, stream):
+    if written and a.overlap:
+        raise VPError("%s: an output shares memory with another one or with another gradient" % name)
+    if a.devices - {torch.cuda.current_device()}:
+        raise VPError("%s: gradients on another device than the current one" % name)
+    _on_current_device((norm, workspace))
+    wp, wb = _ws(workspace)
+    _check(call(load_library(), _ptr(norm, "norm", (torch.float32,), (1,)), wp, wb, _stream(stream)), name)
+
+
+def _gradients(grads, outs=None) -> GradientArguments:
+    if not isinstance(grads, GradientArguments):
+        return GradientArguments(grads, outs)
+    if outs is not None:
+        raise VPError("outs belong to the GradientArguments")
+    return grads
+
+
+def vp_grad_workspace_bytes(n: int) -> int:
+    b = load_library().vp_grad_workspace_bytes(n)
+    if b == ctypes.c_size_t(-1).value:
+        raise VPError("vp_grad_workspace_bytes: invalid arguments")
+    return b
+
+
+def vp_grad_norm(grads, norm, workspace, stream=None) -> None:
+    """norm[0] = the 2-norm of all gradients together.  grads: tensors of fp32 or bf16, or GradientArguments made of them once."""
+    a = _gradients(grads)
+    _grad_call("vp_grad_norm", a, False, lambda lib, np, wp, wb, st: lib.vp_grad_norm(
+        a.ptrs, a.counts, a.dts, a.n, np, wp, wb, st), norm, workspace, stream)
+
+
+def vp_grad_clip(grads, max_norm: float, norm, workspace, outs=None, stream=None) -> None:
+    """vp_grad_norm, and every gradient times max_norm / norm where the norm exceeds max_norm: in place, or into outs.  A norm
+    that is not finite leaves the gradients as they are."""
+    a = _gradients(grads, outs)
+    _grad_call("vp_grad_clip", a, True, lambda lib, np, wp, wb, st: lib.vp_grad_clip(
+        a.ptrs, a.counts, a.dts, a.n, a.out_ptrs, max_norm, np, wp, wb, st), norm, workspace, stream)
+
+
+def vp_grad_scale(grads, max_norm: float, norm, workspace, outs=None, stream=None) -> None:
+    """vp_grad_clip with a norm that is known already."""
+    a = _gradients(grads, outs)
+    _grad_call("vp_grad_scale", a, True, lambda lib, np, wp, wb, st: lib.vp_grad_scale(
+        a.ptrs, a.counts, a.dts, a.n, a.out_ptrs, max_norm, np, wp, wb, st), norm, workspace, stream)
 
 
 def vp_profile_mfma_loop(operands, out, iters: int, blocks: int, stream=None) -> None:

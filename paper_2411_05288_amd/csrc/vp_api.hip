@@ -130,6 +130,21 @@ GemmBf16Params logits_product(const void* H, const int64_t* labels, int64_t N, i
     return g;
 }
 
+bool finite(float v) { return v - v == 0.f; }
+
+// Arguments of the norms around a block that both directions have.
+bool norm_args_ok(const void* y, const void* gate, int64_t gate_rows, const void* w_post, const void* b_post, int64_t N,
+                  uint32_t flags, float scale) {
+    if ((flags & ~(uint32_t)(VP_NORM_POST | VP_NORM_CENTER)) || !finite(scale)) return false;
+    if (gate_rows < 0 || (gate != nullptr) != (gate_rows > 0) || (gate_rows && N % gate_rows)) return false;
+    if (!y && (gate || (flags & VP_NORM_POST))) return false;
+    return (flags & VP_NORM_POST) || (!w_post && !b_post);
+}
+bool norm_sizes_supported(int64_t N, int64_t h) { return N < MAX_ELEMS && h <= MAX_ROW && N * h < MAX_ELEMS; }
+
+// Elements of all gradients together.
+constexpr int64_t MAX_GRAD = (int64_t)1 << 40;
+
 vp_status dev(hipError_t e) { return e == hipSuccess ? VP_OK : VP_ERR_DEVICE; }
 
 // Scratch of vp_output_fwd_noalloc: device memory that belongs to the library's code object, so the
@@ -912,6 +927,90 @@ vp_status vp_embed_bwd(const void* grad_out, const int64_t* ids, int64_t N, int6
                        int64_t shard_offset, vp_dtype dt, float* dtable_shard, void* workspace, size_t workspace_bytes,
                        void* stream) {
     return vp_embed_bwd_group(grad_out, ids, 1, N, h, Vs, shard_offset, dt, &dtable_shard, workspace, workspace_bytes, stream);
+}
+
+// ---- the norms around a block
+
+vp_status vp_block_norm_fwd(const void* x, const void* y, const void* gate, int64_t gate_rows, const void* w_post,
+                            const void* b_post, const void* w, const void* b, int64_t N, int64_t h, vp_dtype dt,
+                            uint32_t flags, float scale, float eps, void* r, void* H, float* stats, void* stream) {
+    if (!x || !H || N < 1 || h < 1 || !dtype_ok(dt)) return VP_ERR_INVALID_ARG;
+    if (!norm_args_ok(y, gate, gate_rows, w_post, b_post, N, flags, scale)) return VP_ERR_INVALID_ARG;
+    if (!(eps > 0.f) || !finite(eps) || (!y && r)) return VP_ERR_INVALID_ARG;
+    for (const void* q : {x, y, gate, w_post, b_post, w, b, (const void*)r, (const void*)H, (const void*)stats})
+        if (!aligned16(q)) return VP_ERR_INVALID_ARG;
+    if (!norm_sizes_supported(N, h)) return VP_ERR_UNSUPPORTED;
+    BlockNorm p{x, y, gate, w_post, b_post, w, b, r, H, stats, (int)N, (int)h, gate_rows, (flags & VP_NORM_POST) != 0,
+                (flags & VP_NORM_CENTER) != 0, scale, eps};
+    return dev(launch_block_norm_fwd(p, dt, (hipStream_t)stream));
+}
+
+size_t vp_block_norm_bwd_workspace_bytes(int64_t N, int64_t h, int64_t gate_rows, uint32_t flags) {
+    if (N < 1 || h < 1 || gate_rows < 0 || (gate_rows && N % gate_rows) || !norm_sizes_supported(N, h)) return (size_t)-1;
+    if (flags & ~(uint32_t)(VP_NORM_POST | VP_NORM_CENTER)) return (size_t)-1;
+    return block_norm_bwd_workspace(N, h, gate_rows, (flags & VP_NORM_POST) != 0);
+}
+
+vp_status vp_block_norm_bwd(const void* dH, vp_dtype dH_dt, const void* dr, const void* r, const void* y, const void* gate,
+                            int64_t gate_rows, const void* w_post, const void* b_post, const void* w, const float* stats,
+                            int64_t N, int64_t h, vp_dtype dt, uint32_t flags, float scale, vp_dtype grad_dt, void* dx,
+                            void* dy, float* dgate, float* dw_post, float* db_post, float* dw, float* db, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+    if (!dH || !r || !stats || !dx || N < 1 || h < 1 || !dtype_ok(dt) || !dtype_ok(dH_dt) || !dtype_ok(grad_dt))
+        return VP_ERR_INVALID_ARG;
+    if (dt == VP_F32 && (dH_dt != VP_F32 || grad_dt != VP_F32)) return VP_ERR_INVALID_ARG;
+    if (!norm_args_ok(y, gate, gate_rows, w_post, b_post, N, flags, scale)) return VP_ERR_INVALID_ARG;
+    if ((y != nullptr) != (dy != nullptr) || (dgate && !gate)) return VP_ERR_INVALID_ARG;
+    if ((dw_post || db_post) && !(flags & VP_NORM_POST)) return VP_ERR_INVALID_ARG;
+    for (const void* q : {dH, dr, r, y, gate, w_post, b_post, w, (const void*)stats, (const void*)dx, (const void*)dy,
+                          (const void*)dgate, (const void*)dw_post, (const void*)db_post, (const void*)dw, (const void*)db,
+                          (const void*)workspace})
+        if (!aligned16(q)) return VP_ERR_INVALID_ARG;
+    if (!norm_sizes_supported(N, h)) return VP_ERR_UNSUPPORTED;
+    const size_t need = vp_block_norm_bwd_workspace_bytes(N, h, gate_rows, flags);
+    if (!workspace || workspace_bytes < need) return VP_ERR_WORKSPACE;
+    BlockNormGrad p{dH, dr, r, y, gate, w_post, b_post, w, stats, dx, dy, dgate, dw_post, db_post, dw, db, (int)N, (int)h,
+                    gate_rows, (flags & VP_NORM_POST) != 0, (flags & VP_NORM_CENTER) != 0, scale};
+    return dev(launch_block_norm_bwd(p, dt, dH_dt, grad_dt, workspace, (hipStream_t)stream));
+}
+
+// ---- the norm of all gradients, and clipping
+
+size_t vp_grad_workspace_bytes(int32_t n) { return n < 0 ? (size_t)-1 : grad_workspace(n); }
+
+static vp_status grad_call(const void* const* grads, const int64_t* counts, const int32_t* dts, int32_t n, void* const* outs,
+                           float max_norm, bool known, float* norm, void* workspace, size_t workspace_bytes, void* stream) {
+    if (n < 0 || !norm || ((uintptr_t)norm & 3u) || (n > 0 && (!grads || !counts || !dts))) return VP_ERR_INVALID_ARG;
+    int64_t total = 0;
+    for (int32_t k = 0; k < n; ++k) {
+        if (counts[k] < 0 || !dtype_ok((vp_dtype)dts[k])) return VP_ERR_INVALID_ARG;
+        if (counts[k] == 0) continue;
+        const uintptr_t mask = dts[k] == VP_BF16 ? 1u : 3u;
+        if (!grads[k] || ((uintptr_t)grads[k] & mask)) return VP_ERR_INVALID_ARG;
+        if (outs && (!outs[k] || ((uintptr_t)outs[k] & mask))) return VP_ERR_INVALID_ARG;
+        if (counts[k] > MAX_GRAD - total) return VP_ERR_UNSUPPORTED;
+        total += counts[k];
+    }
+    if (!aligned16(workspace)) return VP_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < grad_workspace(n)) return VP_ERR_WORKSPACE;
+    return dev(launch_grad(grads, counts, dts, n, outs, max_norm, known, norm, workspace, (hipStream_t)stream));
+}
+
+vp_status vp_grad_norm(const void* const* grads, const int64_t* counts, const int32_t* dts, int32_t n, float* norm,
+                       void* workspace, size_t workspace_bytes, void* stream) {
+    return grad_call(grads, counts, dts, n, nullptr, -1.f, false, norm, workspace, workspace_bytes, stream);
+}
+
+vp_status vp_grad_clip(const void* const* grads, const int64_t* counts, const int32_t* dts, int32_t n, void* const* outs,
+                       float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!(max_norm >= 0.f) || !finite(max_norm)) return VP_ERR_INVALID_ARG;
+    return grad_call(grads, counts, dts, n, outs, max_norm, false, norm, workspace, workspace_bytes, stream);
+}
+
+vp_status vp_grad_scale(const void* const* grads, const int64_t* counts, const int32_t* dts, int32_t n, void* const* outs,
+                        float max_norm, const float* norm, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!(max_norm >= 0.f) || !finite(max_norm)) return VP_ERR_INVALID_ARG;
+    return grad_call(grads, counts, dts, n, outs, max_norm, true, const_cast<float*>(norm), workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

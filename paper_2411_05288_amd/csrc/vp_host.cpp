@@ -8,6 +8,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -95,6 +96,24 @@ PyObject* same_shapes(PyObject*, PyObject* list) {
     Py_RETURN_TRUE;
 }
 
+// on_current_device(tuple of tensors or None) -> True, where all tensors are on the current device
+PyObject* on_current_device(PyObject*, PyObject* ts) {
+    if (!PyTuple_Check(ts)) Py_RETURN_NONE;
+    try {
+        const auto here = c10::hip::current_device();
+        for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(ts); ++i) {
+            PyObject* o = PyTuple_GET_ITEM(ts, i);
+            if (o == Py_None) continue;
+            if (!THPVariable_CheckExact(o)) Py_RETURN_NONE;
+            const at::Tensor& t = THPVariable_Unpack(o);
+            if (!t.defined() || !t.is_cuda() || t.get_device() != here) Py_RETURN_NONE;
+        }
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    Py_RETURN_TRUE;
+}
+
 // stream() -> int: the current stream of the current device
 PyObject* stream(PyObject*, PyObject*) {
     try {
@@ -108,6 +127,7 @@ PyMethodDef methods[] = {
     {"ptr", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(ptr)), METH_FASTCALL, nullptr},
     {"ptrs", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(ptrs)), METH_FASTCALL, nullptr},
     {"same_shapes", same_shapes, METH_O, nullptr},
+    {"on_current_device", on_current_device, METH_O, nullptr},
     {"stream", stream, METH_NOARGS, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

@@ -18,7 +18,8 @@ static inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; 
 // Kernel ids for the optional per-kernel timing (names in vp_profile.hip, same order).
 enum KernelId : int {
     K_GEMM_FWD_STATS = 0, K_GEMM_DLOGITS, K_GEMM_DH, K_GEMM_DW, K_FOLD, K_COMBINE, K_DLOGITS_EW, K_GEMM_F32,
-    K_ROWSTATS_F32, K_EMBED_FWD, K_EMBED_SORT, K_EMBED_ACCUM, K_GEMM_A_ALG2, K_DX_ALG2, K_SUM_SLICES, K_ZERO_PAD, K_COUNT
+    K_ROWSTATS_F32, K_EMBED_FWD, K_EMBED_SORT, K_EMBED_ACCUM, K_GEMM_A_ALG2, K_DX_ALG2, K_SUM_SLICES, K_ZERO_PAD,
+    K_BLOCK_NORM_FWD, K_BLOCK_NORM_BWD, K_GRAD_NORM, K_GRAD_SCALE, K_COUNT
 };
 
 // Brackets the launches made during its lifetime with two events when timing is enabled;
@@ -231,5 +232,36 @@ hipError_t launch_embed_fwd(const void* const* tables, const int64_t* ids, int p
 size_t embed_bwd_workspace(int64_t N, int64_t h, int64_t Vs, int elem_bytes);
 hipError_t launch_embed_bwd(const void* gout, const int64_t* ids, int p, int N, int h, int Vs, int64_t off,
                             int is_bf16, float* const* dtables, void* ws, hipStream_t st);
+
+// The norms around a block.  Pointers as in vp.h; gate_rows > 0 iff gate.
+struct BlockNorm {
+    const void *x, *y, *gate, *w_post, *b_post, *w, *b;
+    void *r, *H;
+    float* stats;
+    int N, h;
+    int64_t gate_rows;
+    int post, center;
+    float scale, eps;
+};
+hipError_t launch_block_norm_fwd(const BlockNorm& p, vp_dtype dt, hipStream_t st);
+
+struct BlockNormGrad {
+    const void *dH, *dr, *r, *y, *gate, *w_post, *b_post, *w;
+    const float* stats;
+    void *dx, *dy;
+    float *dgate, *dw_post, *db_post, *dw, *db;
+    int N, h;
+    int64_t gate_rows;
+    int post, center;
+    float scale;
+};
+size_t block_norm_bwd_workspace(int64_t N, int64_t h, int64_t gate_rows, bool post);
+hipError_t launch_block_norm_bwd(const BlockNormGrad& p, vp_dtype dt, vp_dtype dH_dt, vp_dtype grad_dt, void* workspace,
+                                 hipStream_t st);
+
+// Norm of and scaling by it of n gradients (host arrays as in vp.h).  max_norm < 0: the norm alone; known: the scaling alone.
+size_t grad_workspace(int32_t n);
+hipError_t launch_grad(const void* const* grads, const int64_t* counts, const int32_t* dts, int32_t n, void* const* outs,
+                       float max_norm, bool known, float* norm, void* workspace, hipStream_t st);
 
 }  // namespace vp

@@ -14,7 +14,7 @@ from __future__ import annotations
 
 import contextlib
 from dataclasses import dataclass
-from typing import List, Optional
+from typing import List, Optional, Sequence
 
 import torch
 
@@ -35,6 +35,78 @@ class OutputLayerResult:
     logits: Optional[List[torch.Tensor]]
 
 
+class BlockNormPlan:
+    """Buffers and calls of the norms around a block: r = x + scale * gate * norm(y), H = norm(r) (``post`` norms y, ``center``
+    makes layer norms of RMS norms; y=None: H = norm(x) alone), and the gradients of all of it.
+
+    ``train=False`` keeps no statistics and no buffers for gradients: ``forward`` alone, as for single tokens.  Gradients of
+    activations (dx, dy) are of ``grad_dtype`` (default: the type of x), those of parameters fp32."""
+
+    def __init__(self, x: torch.Tensor, y: Optional[torch.Tensor] = None, *, gate=None, w=None, b=None, w_post=None, b_post=None,
+                 scale: float = 1.0, eps: float = 1e-5, post: bool = False, center: bool = False, grad_dtype=None,
+                 train: bool = True):
+        self.x, self.y = x, y
+        self.N, self.h = x.shape
+        self.gate, self.w, self.b, self.w_post, self.b_post = gate, w, b, w_post, b_post
+        self.scale, self.eps, self.post, self.center = scale, eps, post, center
+        f32 = dict(dtype=torch.float32, device=x.device)
+        self.r = torch.empty_like(x) if y is not None else None
+        self.H = torch.empty_like(x)
+        self.stats = self.dx = self.dy = self.dgate = self.dw = self.db = self.dw_post = self.db_post = self.workspace = None
+        if not train:
+            return
+        self.stats = torch.empty((4, self.N), **f32)
+        self.dx = torch.empty((self.N, self.h), dtype=grad_dtype or x.dtype, device=x.device)
+        self.dy = torch.empty_like(self.dx) if y is not None else None
+        self.dgate, self.dw, self.db, self.dw_post, self.db_post = (
+            None if t is None else torch.empty(t.shape, **f32) for t in (gate, w, b, w_post, b_post))
+        self.workspace = torch.empty((B.vp_block_norm_bwd_workspace_bytes(
+            self.N, self.h, 0 if gate is None else gate.shape[0], post),), dtype=torch.uint8, device=x.device)
+
+    def forward(self, stream=None) -> None:
+        B.vp_block_norm_fwd(self.x, self.y, self.H, r=self.r, stats=self.stats, gate=self.gate, w=self.w, b=self.b,
+                            w_post=self.w_post, b_post=self.b_post, scale=self.scale, eps=self.eps, post=self.post,
+                            center=self.center, stream=stream)
+
+    def backward(self, dH: torch.Tensor, dr: Optional[torch.Tensor] = None, stream=None) -> None:
+        if self.stats is None:
+            raise B.VPError("a plan with train=False has no backward pass")
+        B.vp_block_norm_bwd(dH, self.x if self.r is None else self.r, self.y, self.stats, dx=self.dx, dy=self.dy, dr=dr,
+                            gate=self.gate, w=self.w, w_post=self.w_post, b_post=self.b_post, scale=self.scale, post=self.post,
+                            center=self.center, dgate=self.dgate, dw=self.dw, db=self.db, dw_post=self.dw_post,
+                            db_post=self.db_post, workspace=self.workspace, stream=stream)
+
+    def parameter_gradients(self) -> List[torch.Tensor]:
+        return [t for t in (self.dgate, self.dw, self.db, self.dw_post, self.db_post) if t is not None]
+
+
+class GradientClipPlan:
+    """The norm of many gradients together, and clipping by it: the gradients of all layers of a step, of fp32 or bf16, in place
+    or into ``outs`` (tensors of their types and shapes, views of one flat buffer among them).  The plan keeps the tensors'
+    addresses: a gradient that moves needs a new plan."""
+
+    def __init__(self, grads: List[torch.Tensor], outs: Optional[List[torch.Tensor]] = None):
+        self.arguments = B.GradientArguments(grads, outs)
+        dev = self.arguments.grads[0].device if self.arguments.n else torch.device("cuda", torch.cuda.current_device())
+        self.norm = torch.empty((1,), dtype=torch.float32, device=dev)
+        self.workspace = torch.empty((B.vp_grad_workspace_bytes(self.arguments.n),), dtype=torch.uint8, device=dev)
+
+    def covers(self, grads: List[torch.Tensor]) -> bool:
+        """Whether it was made for exactly these tensors, and they are where they were."""
+        a = self.arguments
+        return a.n == len(grads) and all(g is mine and (g.data_ptr() or None) == p for g, mine, p in zip(grads, a.grads, a.ptrs))
+
+    def compute_norm(self, stream=None) -> None:
+        B.vp_grad_norm(self.arguments, self.norm, self.workspace, stream)
+
+    def clip(self, max_norm: float, stream=None) -> None:
+        B.vp_grad_clip(self.arguments, max_norm, self.norm, self.workspace, stream=stream)
+
+    def scale(self, max_norm: float, norm: Optional[torch.Tensor] = None, stream=None) -> None:
+        """Clips by ``norm`` (default: what compute_norm left, or what the caller made of it, as by a sum over devices)."""
+        B.vp_grad_scale(self.arguments, max_norm, self.norm if norm is None else norm, self.workspace, stream=stream)
+
+
 class OutputLayerPlan:
     """Buffers and launch order for one output-layer workload of p shards.
 
@@ -49,11 +121,20 @@ class OutputLayerPlan:
     4 GiB) and up to 1 GiB of partial sums in ``workspace``; one shard at a time needs the largest
     D alone.  ``workspace_limit`` (bytes) makes the plan go shard by shard where the workspace
     would be larger than that, and so does a device without room for it; with algorithm=2 pass S alone
-    does so where the rest fits."""
+    does so where the rest fits.
 
-    def __init__(self, H: torch.Tensor, W_shards: List[torch.Tensor], labels: torch.Tensor,
+    With ``norm`` (a BlockNormPlan; H is then None) the plan begins with that norm, whose H it reads, and its backward pass
+    ends with the norm's, from dH.  ``clip_gradients`` clips dW and the norm's parameter gradients, and ``others`` with them, by
+    the norm of all of them together."""
+
+    def __init__(self, H: Optional[torch.Tensor], W_shards: List[torch.Tensor], labels: torch.Tensor,
                  save_logits: bool = True, grad_scale: Optional[float] = None, vocab_size: Optional[int] = None,
-                 algorithm: int = 1, workspace_limit: Optional[int] = None):
+                 algorithm: int = 1, workspace_limit: Optional[int] = None,
+                 norm: Optional["BlockNormPlan"] = None):
+        if (H is None) == (norm is None):
+            raise B.VPError("either H or the norm that makes it")
+        self.norm, self.clip_plan = norm, None
+        H = norm.H if H is None else H
         if algorithm not in (1, 2):
             raise B.VPError("algorithm must be 1 (two barriers) or 2 (one barrier)")
         self.algorithm = algorithm
@@ -158,6 +239,8 @@ class OutputLayerPlan:
         return [t if t.shape[0] == v else t[:v] for t, v in zip(tensors, self.valid[:self.live])]
 
     def forward(self, stream=None) -> None:
+        if self.norm is not None:
+            self.norm.forward(stream)
         in_one_call = self.grouped if self.algorithm == 1 else self.grouped_S
         for r in range(self.live if in_one_call else 0, self.p):
             v = self.valid[r]
@@ -235,6 +318,16 @@ class OutputLayerPlan:
                                   self.global_max, self.global_sumexp, self.logits[:q] if self.logits is not None else None,
                                   self.grad_scale, self.dH if self.algorithm == 1 else None,
                                   self._live(self.dW), self.workspace, stream, dh_overwrite=True)
+        if self.norm is not None:
+            self.norm.backward(self.dH, stream=stream)
+
+    def clip_gradients(self, max_norm: float, others: Sequence[torch.Tensor] = (), stream=None) -> torch.Tensor:
+        """Clips in place by the norm of all gradients together, which it returns ([1], on the device)."""
+        grads = self.dW + (self.norm.parameter_gradients() if self.norm is not None else []) + list(others)
+        if self.clip_plan is None or not self.clip_plan.covers(grads):
+            self.clip_plan = GradientClipPlan(grads)
+        self.clip_plan.clip(max_norm, stream)
+        return self.clip_plan.norm
 
     def step(self, stream=None) -> None:
         self.forward(stream)

@@ -1,0 +1,258 @@
+"""The norms around a block (vp_block_norm_fwd, vp_block_norm_bwd) against their formulas in 64 bits, every output element
+within a bound that follows from the roundings of a computation in 32 bits (norm_reference.py)."""
+import itertools
+
+import pytest
+import torch
+
+import norm_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+# lengths from one element to rows that no workgroup holds, odd ones, powers of two and their neighbours
+SIZES = [(1, 1), (3, 7), (70, 8), (5, 63), (5, 64), (129, 65), (1, 128), (128, 256), (33, 511), (34, 1000), (17, 1001), (12, 1024),
+         (64, 2050), (7, 4096), (301, 4096), (9, 4104), (6, 8192), (3, 8200), (5, 12288), (4, 16384), (3, 16391), (2, 32768),
+         (2, 40001), (1, 70000), (1000, 40), (4099, 24)]
+
+
+def guarded(shape, dtype, fill=7.0):
+    """A tensor inside a larger one, and a check that what lies around it stays as it was."""
+    n = 1
+    for s in shape:
+        n *= s
+    pad = 64
+    whole = torch.full((n + 2 * pad,), fill, dtype=dtype, device="cuda")
+    inner = whole[pad:pad + n].view(shape)
+
+    def untouched():
+        return bool((whole[:pad] == fill).all()) and bool((whole[pad + n:] == fill).all())
+    return inner, untouched
+
+
+def inputs(N, h, dtype, post, gate, bias, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+
+    def normal(*shape, std=1.0, mean=0.0):
+        return (torch.randn(*shape, generator=g, device="cuda") * std + mean).to(dtype)
+    return {"x": normal(N, h, mean=0.3), "y": normal(N, h, std=2.0, mean=-0.4), "gate": normal(gate, h, std=0.5, mean=0.2) if gate else None,
+            "w": normal(h, std=0.2, mean=1.0) if seed % 5 else None, "b": normal(h, std=0.3) if bias else None,
+            "w_post": normal(h, std=0.2, mean=1.0) if post and seed % 7 else None, "b_post": normal(h, std=0.3) if post and bias else None}
+
+
+def gates(N):
+    """Rows of a gate: none, one, one for every token, and splits in between."""
+    some = [g for g in range(2, N) if N % g == 0]
+    return [0, 1, N] + some[:1] + some[-1:] + some[len(some) // 2:len(some) // 2 + 1]
+
+
+def variants():
+    out = []
+    for k, (N, h) in enumerate(SIZES):
+        for j, (dtype, post, center) in enumerate(itertools.product((BF16, F32), (True, False), (True, False))):
+            gs = gates(N)
+            out.append((N, h, dtype, post, center, gs[(k + j) % len(gs)], (k + j // 2) % 2 == 0, 10 * k + j))
+    return out
+
+
+@pytest.mark.parametrize("N,h,dtype,post,center,gate,bias,seed", variants())
+def test_forward_and_backward(N, h, dtype, post, center, gate, bias, seed):
+    import paper_2411_05288_amd as vp
+    s = inputs(N, h, dtype, post, gate, bias, seed)
+    scale, eps = (1.0, 0.37, -1.25)[seed % 3], (1e-5, 1e-6, 0.1)[seed % 3]
+    opts = dict(gate=s["gate"], w_post=s["w_post"], b_post=s["b_post"], scale=scale, post=post, center=center)
+    (H, H_ok), (r, r_ok), (stats, s_ok) = guarded((N, h), dtype), guarded((N, h), dtype), guarded((4, N), F32)
+    vp.vp_block_norm_fwd(s["x"], s["y"], H, r=r, stats=stats, w=s["w"], b=s["b"], eps=eps, **opts)
+    for name, (value, bound) in ref.forward(s["x"], s["y"], w=s["w"], b=s["b"], eps=eps, **opts).items():
+        ref.check(name, {"r": r, "H": H, "stats": stats}[name], value, bound)
+    assert H_ok() and r_ok() and s_ok()
+
+    dH_type = (F32, dtype)[seed % 2]
+    grad = (dtype, F32)[seed // 2 % 2]
+    g = torch.Generator(device="cuda").manual_seed(seed + 1)
+    dH = torch.randn(N, h, generator=g, device="cuda").to(dH_type)
+    dr = torch.randn(N, h, generator=g, device="cuda").to(grad) if seed % 4 else None
+    want = ["dx", "dy", "dw", "db"] + (["dgate"] if gate else []) + (["dw_post", "db_post"] if post else [])
+    shapes = {"dx": ((N, h), grad), "dy": ((N, h), grad), "dgate": ((gate, h), F32)}
+    out = {k: guarded(*shapes.get(k, ((h,), F32))) for k in want}
+    ws = torch.full((vp.vp_block_norm_bwd_workspace_bytes(N, h, gate, post),), 0xFF, dtype=torch.uint8, device="cuda")
+    vp.vp_block_norm_bwd(dH, r, s["y"], stats, dr=dr, w=s["w"], workspace=ws, **{k: t for k, (t, _) in out.items()}, **opts)
+    expected = ref.backward(dH, r, s["y"], stats, dr=dr, w=s["w"], grad_dtype=grad, **opts)
+    assert sorted(expected) == sorted(want)
+    for name, (value, bound) in expected.items():
+        ref.check(name, out[name][0], value, bound)
+        assert out[name][1](), name
+    # the same again: bit for bit
+    again = {k: torch.empty_like(t) for k, (t, _) in out.items()}
+    vp.vp_block_norm_bwd(dH, r, s["y"], stats, dr=dr, w=s["w"], workspace=ws, **again, **opts)
+    for k, t in again.items():
+        assert torch.equal(t, out[k][0]), k
+
+
+@pytest.mark.parametrize("N,h,dtype,center", [(1, 4096, BF16, False), (5, 1001, F32, True), (130, 320, BF16, True), (2, 33333, BF16, False)])
+def test_norm_alone(N, h, dtype, center):
+    import paper_2411_05288_amd as vp
+    s = inputs(N, h, dtype, False, 0, True, 3)
+    H, stats = torch.empty_like(s["x"]), torch.empty(4, N, device="cuda")
+    vp.vp_block_norm_fwd(s["x"], None, H, stats=stats, w=s["w"], b=s["b"], center=center)
+    expected = ref.forward(s["x"], w=s["w"], b=s["b"], center=center)
+    ref.check("H", H, *expected["H"])
+    ref.check("stats", stats, *expected["stats"])
+    bare = torch.empty_like(H)      # serving: nothing kept
+    vp.vp_block_norm_fwd(s["x"], None, bare, w=s["w"], b=s["b"], center=center)
+    assert torch.equal(bare, H)
+    dH, dx, dw = torch.randn(N, h, device="cuda"), torch.empty(N, h, device="cuda"), torch.empty(h, device="cuda")
+    ws = torch.full((vp.vp_block_norm_bwd_workspace_bytes(N, h),), 0xFF, dtype=torch.uint8, device="cuda")
+    vp.vp_block_norm_bwd(dH, s["x"], None, stats, dx=dx, w=s["w"], dw=dw, center=center, workspace=ws)
+    expected = ref.backward(dH, s["x"], None, stats, w=s["w"], center=center)
+    ref.check("dx", dx, *expected["dx"])
+    ref.check("dw", dw, *expected["dw"])
+
+
+@pytest.mark.parametrize("N,h", [(9, 1000), (3, 4096), (2, 40000)])
+def test_in_place(N, h):
+    import paper_2411_05288_amd as vp
+    s = inputs(N, h, BF16, True, 1, True, 4)
+    opts = dict(gate=s["gate"], w_post=s["w_post"], b_post=s["b_post"], post=True, scale=0.5)
+    H, r, stats = torch.empty_like(s["x"]), torch.empty_like(s["x"]), torch.empty(4, N, device="cuda")
+    vp.vp_block_norm_fwd(s["x"], s["y"], H, r=r, stats=stats, w=s["w"], b=s["b"], **opts)
+    x, y = s["x"].clone(), s["y"].clone()
+    vp.vp_block_norm_fwd(x, y, y, r=x, w=s["w"], b=s["b"], **opts)
+    assert torch.equal(x, r) and torch.equal(y, H)
+    dH, dr = torch.randn(N, h, device="cuda").bfloat16(), torch.randn(N, h, device="cuda").bfloat16()
+    ws = torch.empty(vp.vp_block_norm_bwd_workspace_bytes(N, h, 1, post=True), dtype=torch.uint8, device="cuda")
+
+    def back(dr, dx):
+        out = {"dx": dx, "dy": torch.empty_like(dx), "dgate": torch.empty(1, h, device="cuda"), "dw": torch.empty(h, device="cuda")}
+        vp.vp_block_norm_bwd(dH, r, s["y"], stats, dr=dr, w=s["w"], workspace=ws, **out, **opts)
+        return out
+    apart = back(dr, torch.empty_like(dr))
+    inside = back(dr, dr)
+    for k in apart:
+        assert torch.equal(apart[k], inside[k]), k
+
+
+@pytest.mark.parametrize("N,h,gate", [(6, 96, 3), (4, 1000, 1)])
+@pytest.mark.parametrize("center", [True, False])
+def test_gradients_against_differences(N, h, gate, center):
+    """Directional derivatives of <dH, H> + <dr, r> by central differences of the forward formulas in 64 bits."""
+    import paper_2411_05288_amd as vp
+    s = inputs(N, h, F32, True, gate, True, 11)
+    leaves = ["x", "y", "gate", "w", "b", "w_post", "b_post"]
+    opts = dict(scale=0.7, post=True, center=center)
+    H, r, stats = torch.empty_like(s["x"]), torch.empty_like(s["x"]), torch.empty(4, N, device="cuda")
+    vp.vp_block_norm_fwd(s["x"], s["y"], H, r=r, stats=stats, gate=s["gate"], w=s["w"], b=s["b"], w_post=s["w_post"],
+                         b_post=s["b_post"], **opts)
+    dH, dr = torch.randn(N, h, device="cuda"), torch.randn(N, h, device="cuda")
+    names = {"x": "dx", "y": "dy", "gate": "dgate", "w": "dw", "b": "db", "w_post": "dw_post", "b_post": "db_post"}
+    out = {names[k]: torch.empty_like(s[k]) for k in leaves}
+    ws = torch.empty(vp.vp_block_norm_bwd_workspace_bytes(N, h, gate, post=True), dtype=torch.uint8, device="cuda")
+    vp.vp_block_norm_bwd(dH, r, s["y"], stats, dr=dr, gate=s["gate"], w=s["w"], w_post=s["w_post"], b_post=s["b_post"],
+                         workspace=ws, **out, **opts)
+    expected = ref.backward(dH, r, s["y"], stats, dr=dr, gate=s["gate"], w=s["w"], w_post=s["w_post"], b_post=s["b_post"], **opts)
+    p = {k: s[k].double() for k in leaves}
+
+    def loss(q):      # the forward formulas, from inputs in 64 bits
+        o = ref.forward(**{**q}, **opts)
+        return float((o["H"][0] * dH.double()).sum() + (o["r"][0] * dr.double()).sum())
+    ref.HALF.setdefault(torch.float64, 0.0)
+    for k in leaves:
+        way = torch.randn(p[k].shape, device="cuda", dtype=torch.float64)
+        e = 1e-5
+        # central differences: truncation of order e^2, rounding of order 1e-16 / e
+        slope = (loss({**p, k: p[k] + e * way}) - loss({**p, k: p[k] - e * way})) / (2 * e)
+        got = float((out[names[k]].double() * way).sum())
+        # every element of the gradient is within its bound; r and the statistics that the kernel read are rounded to 32 bits
+        # (a relative change of the gradient of some 2^-23 for each of six uses), and the differences are good to 1e-7
+        value, bound = expected[names[k]]
+        room = float((bound * way.abs()).sum()) + float((value * way).abs().sum()) * (6 * 2.0 ** -23 + 1e-7) + 1e-6
+        assert abs(got - slope) <= room, (k, got, slope, room)
+
+
+def test_nan_and_inf_stay_in_their_rows():
+    import paper_2411_05288_amd as vp
+    N, h = 8, 1000
+    s = inputs(N, h, BF16, True, 0, False, 1)
+    clean = {k: v.clone() for k, v in s.items() if v is not None}
+    s["x"][2, 5], s["y"][4, 7], s["x"][6, 0] = float("nan"), float("inf"), float("-inf")
+    outs = []
+    for q in (clean, s):
+        H, r, stats = torch.empty_like(s["x"]), torch.empty_like(s["x"]), torch.empty(4, N, device="cuda")
+        vp.vp_block_norm_fwd(q["x"], q["y"], H, r=r, stats=stats, w=s["w"], w_post=s["w_post"], post=True)
+        outs.append((H, r, stats))
+    for row in range(N):
+        same = [torch.equal(a[row], b[row]) for a, b in zip(outs[0][:2], outs[1][:2])] + [torch.equal(outs[0][2][:, row], outs[1][2][:, row])]
+        assert all(same) if row not in (2, 4, 6) else not all(same), row
+    assert bool(torch.isnan(outs[1][0][2]).any())
+
+
+def test_zero_rows_and_gates():
+    import paper_2411_05288_amd as vp
+    N, h = 4, 640
+    x = torch.zeros(N, h, device="cuda")
+    H = torch.full_like(x, 7.0)
+    stats = torch.empty(4, N, device="cuda")
+    vp.vp_block_norm_fwd(x, None, H, stats=stats, eps=1e-6)
+    assert bool((H == 0).all()) and torch.allclose(stats[3], torch.full((N,), 1e3, device="cuda"), rtol=1e-6)
+    y = torch.randn(N, h, device="cuda")
+    r = torch.empty_like(x)
+    x = torch.randn(N, h, device="cuda")
+    vp.vp_block_norm_fwd(x, y, H, r=r, gate=torch.zeros(1, h, device="cuda"), post=True)
+    assert torch.equal(r, x)
+
+
+def test_other_stream_and_graph():
+    import paper_2411_05288_amd as vp
+    N, h, G = 60, 1032, 5
+    s = inputs(N, h, BF16, True, G, True, 2)
+    plan = vp.BlockNormPlan(s["x"], s["y"], gate=s["gate"], w=s["w"], b=s["b"], w_post=s["w_post"], b_post=s["b_post"], scale=0.5,
+                            post=True, center=True)
+    dH, dr = torch.randn(N, h, device="cuda"), torch.randn(N, h, device="cuda").bfloat16()
+    outs = [plan.r, plan.H, plan.stats, plan.dx, plan.dy] + plan.parameter_gradients()
+
+    def step(stream=None):
+        plan.forward(stream)
+        plan.backward(dH, dr, stream)
+    step()
+    torch.cuda.synchronize()
+    expected = [t.clone() for t in outs]
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):
+        for t in outs:
+            t.fill_(float("nan"))
+        torch.cuda.synchronize()
+        step(stream)
+        side.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, expected))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        for t in outs + [plan.workspace]:
+            t.fill_(float("nan") if t.is_floating_point() else 0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, expected))
+        assert float(torch.arange(1000, device="cuda", dtype=torch.float32).sum()) == 499500.0
+
+
+def test_gradients_that_are_not_wanted():
+    import paper_2411_05288_amd as vp
+    N, h = 50, 1200
+    s = inputs(N, h, BF16, True, 10, True, 8)
+    opts = dict(gate=s["gate"], w_post=s["w_post"], b_post=s["b_post"], post=True, center=True)
+    H, r, stats = torch.empty_like(s["x"]), torch.empty_like(s["x"]), torch.empty(4, N, device="cuda")
+    vp.vp_block_norm_fwd(s["x"], s["y"], H, r=r, stats=stats, w=s["w"], b=s["b"], **opts)
+    dH = torch.randn(N, h, device="cuda")
+    ws = torch.empty(vp.vp_block_norm_bwd_workspace_bytes(N, h, 10, post=True), dtype=torch.uint8, device="cuda")
+    every = {"dgate": (10, h), "dw": (h,), "db": (h,), "dw_post": (h,), "db_post": (h,)}
+    results = []
+    for names in [list(every)] + [[k] for k in every] + [[]]:
+        out = {k: torch.empty(every[k], device="cuda") for k in names}
+        out["dx"], out["dy"] = torch.empty_like(r), torch.empty_like(r)
+        ws.fill_(0xFF)
+        vp.vp_block_norm_bwd(dH, r, s["y"], stats, w=s["w"], workspace=ws, **out, **opts)
+        results.append(out)
+        for k in out:
+            assert torch.equal(out[k], results[0][k]), (names, k)

@@ -1,0 +1,229 @@
+"""The norm of many gradients together and clipping by it (vp_grad_norm, vp_grad_clip, vp_grad_scale) against sums in 64 bits."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+HALF = {F32: 2.0 ** -24, BF16: 2.0 ** -8}
+
+
+def lists():
+    """(name, [(elements, type, elements that it starts behind an aligned address)])"""
+    chunk = 32768
+    yield "none", []
+    yield "one", [(1, F32, 0)]
+    yield "empty tensors", [(0, F32, 0), (0, BF16, 0)]
+    yield "empty ones between", [(0, F32, 0), (5, F32, 0), (0, BF16, 0), (0, F32, 0), (9, BF16, 0), (0, F32, 0)]
+    yield "odd starts", [(n, t, k) for n in (1, 3, 4, 8, 17, 1000, 8192, 20011) for t in (F32, BF16) for k in (1, 2, 3)]
+    yield "around a chunk", [(chunk // s + d, t, 0) for t, s in ((F32, 4), (BF16, 2)) for d in (-9, -8, -4, -1, 0, 1, 7, 8)]
+    yield "as many as the arguments hold", [(k % 37 + 1, (F32, BF16)[k % 2], 0) for k in range(120)]
+    yield "one more", [(k % 37 + 1, (F32, BF16)[k % 2], k % 3) for k in range(121)]
+    yield "many", [(k * k % 4001, (F32, BF16)[k % 3 == 0], k % 2) for k in range(700)]
+    yield "more chunks than workgroups", [(20000003, F32, 0), (7, BF16, 1), (30000001, BF16, 3)]
+
+
+def make(spec, seed=0, std=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    out = []
+    for n, t, k in spec:
+        whole = torch.full((n + k + 64,), 7.0, dtype=t, device="cuda")
+        whole[k:k + n] = (torch.randn(n, generator=g, device="cuda") * std).to(t)
+        out.append((whole, whole[k:k + n]))
+    return out
+
+
+def exact_norm(grads):
+    return math.sqrt(math.fsum(float(g.double().square().sum()) for g in grads))
+
+
+def check_clipped(got, grad, factor):
+    # norm to half a step, the quotient, the product: three roundings to 32 bits, and the last one to the type
+    value = grad.double() * factor
+    bound = value.abs() * (4 * 2.0 ** -24 + (HALF[grad.dtype] if grad.dtype == BF16 else 0)) + 1e-44 + (5e-41 if grad.dtype == BF16 else 0)
+    assert bool(((got.double() - value).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("name,spec", list(lists()), ids=[n for n, _ in lists()])
+@pytest.mark.parametrize("max_norm", [0.25, 1e9, 0.0])
+def test_norm_clip_and_scale(name, spec, max_norm):
+    import paper_2411_05288_amd as vp
+    both = make(spec, seed=len(spec))
+    grads = [g for _, g in both]
+    before = [g.clone() for g in grads]
+    expected = exact_norm(grads)
+    norm = torch.full((1,), 7.0, device="cuda")
+    ws = torch.full((vp.vp_grad_workspace_bytes(len(grads)),), 0xFF, dtype=torch.uint8, device="cuda")
+    vp.vp_grad_norm(grads, norm, ws)
+    # the sum in 64 bits, its root rounded to 32
+    assert abs(float(norm) - expected) <= expected * (2.0 ** -24 + 1e-12)
+    first = norm.clone()
+    factor = max_norm / expected if expected > max_norm else 1.0
+    # into other tensors
+    outs = make(spec, seed=99)
+    ws.fill_(0xFF)
+    norm.fill_(7.0)
+    vp.vp_grad_clip(grads, max_norm, norm, ws, outs=[o for _, o in outs])
+    assert torch.equal(norm, first)
+    for (whole, o), (n, t, k), g, b in zip(outs, spec, grads, before):
+        assert torch.equal(g, b)
+        check_clipped(o, g, factor)
+        assert bool((whole[:k] == 7).all()) and bool((whole[k + n:] == 7).all())
+    # in place, and by a norm that is known
+    for known in (False, True):
+        here = make(spec, seed=len(spec))
+        if known:
+            vp.vp_grad_scale([g for _, g in here], max_norm, norm, ws)
+        else:
+            vp.vp_grad_clip([g for _, g in here], max_norm, norm, ws)
+        assert torch.equal(norm, first)
+        for (whole, g), (_, o), (n, t, k) in zip(here, outs, spec):
+            assert torch.equal(g, o)
+            assert bool((whole[:k] == 7).all()) and bool((whole[k + n:] == 7).all())
+
+
+def test_repeated_and_in_another_order():
+    """The norm does not depend on how often it is taken, and the tensors' order changes it by a rounding at most."""
+    import paper_2411_05288_amd as vp
+    grads = [g for _, g in make([(50000, F32, 0), (70001, BF16, 1), (3, F32, 2)], seed=5)]
+    ws = torch.empty(vp.vp_grad_workspace_bytes(3), dtype=torch.uint8, device="cuda")
+    norms = []
+    for order in (grads, grads, grads[::-1]):
+        norm = torch.empty(1, device="cuda")
+        vp.vp_grad_norm(order, norm, ws)
+        norms.append(norm)
+    assert torch.equal(norms[0], norms[1])
+    assert abs(float(norms[0]) - float(norms[2])) <= 2.0 ** -23 * float(norms[0])
+
+
+@pytest.mark.parametrize("value", [1e-30, 1e30, 3e38])
+def test_squares_beyond_the_range_of_32_bits(value):
+    import paper_2411_05288_amd as vp
+    n = 1000
+    g = torch.full((n,), value, device="cuda")
+    norm, ws = torch.empty(1, device="cuda"), torch.empty(vp.vp_grad_workspace_bytes(1), dtype=torch.uint8, device="cuda")
+    vp.vp_grad_clip([g], 1.0, norm, ws)
+    expected = float(torch.tensor(value)) * math.sqrt(n)
+    if expected > 3.4028235e38:      # the norm is beyond 32 bits: it says so, and the gradients stay
+        assert math.isinf(float(norm)) and bool((g == value).all())
+    else:
+        assert abs(float(norm) - expected) <= 2.0 ** -23 * expected
+        assert bool(torch.isfinite(g).all()) and abs(float(g[0]) - min(float(torch.tensor(value)), 1 / math.sqrt(n))) <= 1e-6 / math.sqrt(n)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("where", [0, 12345, 39999])
+def test_a_norm_that_is_not_finite_leaves_the_gradients(bad, where):
+    import paper_2411_05288_amd as vp
+    for dtype in (F32, BF16):
+        grads = [torch.randn(40000, device="cuda").to(dtype), torch.randn(33, device="cuda")]
+        grads[0][where] = bad
+        before = [g.clone() for g in grads]
+        outs = [torch.empty_like(g) for g in grads]
+        plan, copy = vp.GradientClipPlan(grads), vp.GradientClipPlan(grads, outs)
+        plan.clip(1.0)
+        copy.clip(1.0)
+        assert not math.isfinite(float(plan.norm)) and (math.isnan(bad) == math.isnan(float(plan.norm)))
+        for g, b, o in zip(grads, before, outs):
+            assert torch.equal(g.view(torch.int16 if g.dtype == BF16 else torch.int32), b.view(torch.int16 if g.dtype == BF16 else torch.int32))
+            assert torch.equal(torch.isnan(o), torch.isnan(b)) and torch.equal(o[~torch.isnan(o)], b[~torch.isnan(b)])
+
+
+def test_plan_on_another_stream_and_in_a_graph():
+    import paper_2411_05288_amd as vp
+    spec = [(k * 977 % 50021, (F32, BF16)[k % 2], k % 2) for k in range(150)]
+    grads, outs = [g for _, g in make(spec, seed=1)], [o for _, o in make(spec, seed=2)]
+    plan = vp.GradientClipPlan(grads, outs)
+    plan.clip(0.5)
+    torch.cuda.synchronize()
+    expected, norm = [o.clone() for o in outs], plan.norm.clone()
+    side = torch.cuda.Stream()
+
+    def clear():
+        for o in outs:
+            o.fill_(9.0)
+        plan.norm.fill_(9.0)
+        plan.workspace.fill_(0xFF)
+        torch.cuda.synchronize()
+    clear()
+    plan.clip(0.5, stream=side)
+    side.synchronize()
+    assert torch.equal(plan.norm, norm) and all(torch.equal(a, b) for a, b in zip(outs, expected))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        plan.clip(0.5)
+    # the calls' host arrays are gone from the plan when the graph is replayed
+    plan.arguments.ptrs = plan.arguments.counts = plan.arguments.out_ptrs = None
+    for _ in range(3):
+        clear()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(plan.norm, norm) and all(torch.equal(a, b) for a, b in zip(outs, expected))
+        assert float(torch.arange(1000, device="cuda", dtype=torch.float32).sum()) == 499500.0
+
+
+def test_shared_memory_is_refused():
+    import paper_2411_05288_amd as vp
+    whole = torch.randn(1000, device="cuda")
+    norm, ws = torch.empty(1, device="cuda"), torch.empty(vp.vp_grad_workspace_bytes(8), dtype=torch.uint8, device="cuda")
+    before = whole.clone()
+    a, b = whole[:600], whole[500:]
+    for grads, outs in (([whole, whole], None), ([a, b], None), ([whole[:10], whole[20:30]], [whole[40:50], whole[45:55]]),
+                        ([whole[:10], whole[20:30]], [whole[40:50], whole[5:15]]), ([whole[:10]], [whole[1:11]]),
+                        ([whole[:10], whole[20:30]], [whole[20:30], whole[:10]])):
+        with pytest.raises(vp.VPError, match="shares memory"):
+            vp.vp_grad_clip(grads, 0.1, norm, ws, outs=outs)
+    torch.cuda.synchronize()
+    assert torch.equal(whole, before)
+    vp.vp_grad_norm([whole, whole], norm, ws)      # reading a tensor twice is no conflict
+    assert abs(float(norm) - math.sqrt(2) * float(whole.double().norm())) <= 1e-6 * float(norm)
+    vp.vp_grad_clip([whole[:10], whole[20:30]], 0.1, norm, ws, outs=[whole[:10], whole[20:30]])      # in place by outs
+
+
+def test_training_step_from_norm_to_clipping():
+    """The last block's norms, the sharded output layer, their gradients, the input layer's, and clipping over all of them."""
+    import norm_reference as ref
+    import paper_2411_05288_amd as vp
+    N, h, V, p = 96, 256, 1000, 4
+    g = torch.Generator(device="cuda").manual_seed(3)
+
+    def normal(*shape, std=1.0, mean=0.0):
+        return torch.randn(*shape, generator=g, device="cuda") * std + mean
+    x, y, w, wp = normal(N, h), normal(N, h), normal(h, std=0.1, mean=1.0), normal(h, std=0.1, mean=1.0)
+    Ws = [normal(V // p, h, std=0.05) for _ in range(p)]
+    ids = torch.randint(0, V, (N,), generator=g, device="cuda")
+    labels = torch.randint(0, V, (N,), generator=g, device="cuda")
+    norm = vp.BlockNormPlan(x, y, w=w, w_post=wp, post=True)
+    plan = vp.OutputLayerPlan(None, Ws, labels, norm=norm)
+    plan.step()
+    embed = vp.EmbeddingPlan([torch.zeros(V // p, h, device="cuda") for _ in range(p)], ids, norm.dx)
+    embed.backward()
+    # the same in 64 bits, by automatic differentiation of the formulas
+    leaves = [t.double().requires_grad_() for t in (x, y, w, wp)] + [W.double().requires_grad_() for W in Ws]
+    X, Y, W1, WP = leaves[:4]
+
+    def rms(v):
+        return v / (v.square().mean(1, keepdim=True) + norm.eps).sqrt()
+    logits = rms(X + rms(Y) * WP) * W1 @ torch.cat(leaves[4:]).t()
+    loss = (torch.logsumexp(logits, 1) - logits.gather(1, labels[:, None])[:, 0]).mean()
+    loss.backward()
+    table = torch.zeros(V, h, device="cuda", dtype=torch.float64).index_add_(0, ids, X.grad)
+    # the products of the fp32 path keep 1e-5 of a tensor's largest element, and so does what is made of them
+    assert abs(float(plan.loss) - float(loss.detach())) <= 1e-5 * float(loss.detach())
+    grads = [*plan.dW, norm.dw, norm.dw_post, *embed.dtable]
+    expected = [*[t.grad for t in leaves[4:]], W1.grad, WP.grad, *table.split(V // p)]
+    for name, got, value in [("dx", norm.dx, X.grad), ("dy", norm.dy, Y.grad)] + [(str(k), a, b) for k, (a, b) in enumerate(zip(grads, expected))]:
+        assert float((got.double() - value).abs().max()) <= 2e-5 * float(value.abs().max()), name
+    before = [t.clone() for t in grads]
+    total = exact_norm(before)
+    got = plan.clip_gradients(total / 3, embed.dtable)
+    assert abs(float(got) - total) <= 2.0 ** -23 * total
+    for a, b in zip(grads, before):
+        check_clipped(a, b, 1 / 3)
+    plan.step()      # the next step writes the same gradients again, and the same plan clips them
+    first = plan.clip_plan
+    embed.dtable[0].mul_(3.0)
+    plan.clip_gradients(total / 3, embed.dtable)
+    assert plan.clip_plan is first
