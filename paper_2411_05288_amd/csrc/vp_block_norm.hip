@@ -91,6 +91,7 @@ __global__ __launch_bounds__(TR <= 64 ? 256 : TR) void block_norm_fwd_kernel(Blo
     __shared__ float sh[2][K_ROW_SUMS];
     int turn = 0;
     constexpr int ROWS = TR <= 64 ? 256 / TR : 1;
+    constexpr bool EARLY = TR < 1024;      // (of the longest rows two workgroups fit a CU without)
     const int t = threadIdx.x % TR, threads = TR <= 64 ? TR : blockDim.x, row = blockIdx.x * ROWS + threadIdx.x / TR;
     const bool live = row < p.N;
     const int i = live ? row : p.N - 1;      // (a workgroup's rows past the last one take part in nothing but the sums)
@@ -109,15 +110,17 @@ __global__ __launch_bounds__(TR <= 64 ? 256 : TR) void block_norm_fwd_kernel(Blo
         if (y) ry[c] = load8(y + at, j[c]);
         if (gate) rg[c] = load8(gate, j[c]);
     }
-    // (asked for before the first sum: after it, they would be waited for)
+    auto load_post = [&](int c) {
+        wp[c] = load8((const T*)p.w_post, j[c], 1.f);
+        bp[c] = load8((const T*)p.b_post, j[c]);
+    };
+    // asked for before the first sum, as after it they would be waited for
+    if constexpr (EARLY)
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        if (p.post) {
-            wp[c] = load8((const T*)p.w_post, j[c], 1.f);
-            bp[c] = load8((const T*)p.b_post, j[c]);
+        for (int c = 0; c < C; ++c) {
+            if (p.post) load_post(c);
+            w[c] = load8((const T*)p.w, j[c], 1.f);
         }
-        w[c] = load8((const T*)p.w, j[c], 1.f);
-    }
     // the mean and the deviation of what v holds: squares of differences to the mean, which has been summed first
     auto statistics = [&]() {
         Normed m{0.f, 0.f};
@@ -153,9 +156,11 @@ __global__ __launch_bounds__(TR <= 64 ? 256 : TR) void block_norm_fwd_kernel(Blo
     }
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        if (p.post)
+        if (p.post) {
+            if constexpr (!EARLY) load_post(c);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[c][e] = (v[c][e] - a.m) * a.rho * wp[c][e] + bp[c][e];
+        }
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[c][e] = y ? rx[c][e] + (gate ? p.scale * rg[c][e] : p.scale) * v[c][e] : rx[c][e];
         if (p.r && live) store8((T*)p.r + at, j[c], skip[c], v[c]);
@@ -163,6 +168,7 @@ __global__ __launch_bounds__(TR <= 64 ? 256 : TR) void block_norm_fwd_kernel(Blo
     const Normed m = statistics();
 #pragma unroll
     for (int c = 0; c < C; ++c) {
+        if constexpr (!EARLY) w[c] = load8((const T*)p.w, j[c], 1.f);
         const Raw8<T> b = load8((const T*)p.b, j[c]);
         float o[8];
 #pragma unroll
@@ -368,11 +374,6 @@ ColumnSums cut(int64_t N, int64_t h, int64_t gate_rows) {
     return s;
 }
 
-#ifndef FWD1
-#define FWD1 4096
-#define FWD2 8192
-#define FWD4 8192
-#endif
 constexpr int MAX_ROW_BLOCKS = 1 << 16;
 
 }  // namespace
@@ -390,9 +391,9 @@ hipError_t launch_block_norm_fwd(const BlockNorm& p, vp_dtype dt, hipStream_t st
     if (p.h >= MIN_COLUMNS) {
         if (p.h <= 128) VP_FWD(16, 1, 256);
         if (p.h <= 512) VP_FWD(64, 1, 256);
-        if (p.h <= FWD1) VP_FWD(512, 1, (int)ceil_div(p.h, 512) * 64);
-        if (p.h <= FWD2) VP_FWD(512, 2, (int)ceil_div(p.h, 1024) * 64);
-        if (p.h <= FWD4) VP_FWD(512, 4, (int)ceil_div(p.h, 2048) * 64);
+        if (p.h <= 1024) VP_FWD(64, 2, 256);
+        if (p.h <= 2048) VP_FWD(256, 1, (int)ceil_div(p.h, 512) * 64);
+        if (p.h <= 8192) VP_FWD(512, 2, (int)ceil_div(p.h, 1024) * 64);
         if (p.h <= 16384) VP_FWD(1024, 2, (int)ceil_div(p.h, 1024) * 64);
     }
 #undef VP_FWD

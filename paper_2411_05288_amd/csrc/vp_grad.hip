@@ -9,32 +9,47 @@
 // Squares are formed and summed in fp64: an fp32 value's square is exact there and neither over- nor underflows, and the sum
 // of 10^9 of them keeps all digits that the fp32 result has.  Order of the sum: every thread its elements in ascending order,
 // then fixed trees over the workgroup and over the workgroups' partial sums; no atomics.
+#include <limits.h>
+
 #include "vp_internal.h"
 
 namespace vp {
 
 namespace {
 
-constexpr int GRAD_LIST = 120;              // tensors in the kernel arguments
-constexpr int GRAD_CHUNK_BYTES = 32768;
+constexpr int GRAD_LIST = 160;              // tensors in the kernel arguments
+constexpr int GRAD_CHUNK_BYTES = 32768;     // 256 threads, eight loads of 16 bytes each
 constexpr int GRAD_BLOCKS = 1024;           // partial sums at most
+constexpr int GRAD_FIRSTS = 2048;           // numbers of first chunks that a workgroup holds in LDS
 
 struct GradTensor {
     const void* g;
     void* o;
-    int64_t count;
-    int first;          // number of its first chunk
-    int bf16;
+    uint64_t size;      // elements * 2, + 1 with bf16
+    __host__ __device__ bool bf16() const { return size & 1; }
+    __host__ __device__ int64_t count() const { return (int64_t)(size >> 1); }
+    __host__ __device__ int64_t bytes() const { return count() * (bf16() ? 2 : 4); }
+    __host__ __device__ int chunks() const { return (int)((bytes() + GRAD_CHUNK_BYTES - 1) / GRAD_CHUNK_BYTES); }
 };
 struct GradList {
     int n;              // tensors here
-    int at;             // table: number of the first of them
+    int at, first;      // table: number of the first of them, and of its first chunk
     GradTensor t[GRAD_LIST];
+};
+struct GradTable {      // more tensors than the arguments hold: entries and the number of the first chunk of each
+    GradTensor* t;
+    int* first;
 };
 
 // Element-aligned vectors of 16 bytes: gradients may be views that start anywhere.
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef unsigned short u16x8u __attribute__((ext_vector_type(8), aligned(2)));
+
+// (an address from the table is one of global memory)
+template <typename T>
+__device__ __forceinline__ T* global(T* p) {
+    return (T*)(__attribute__((address_space(1))) T*)p;
+}
 
 __device__ __forceinline__ double wave_sum64(double v) {
 #pragma unroll
@@ -48,15 +63,83 @@ __device__ __forceinline__ double block_sum64(double v, double* sh) {      // 25
     return (sh[0] + sh[1]) + (sh[2] + sh[3]);
 }
 
-// The tensor of chunk c: the last one whose first chunk is not behind it (tensors without elements have no chunks).
-__device__ __forceinline__ int tensor_of(const GradTensor* t, int n, int c) {
-    int lo = 0, hi = n - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (t[mid].first <= c) lo = mid; else hi = mid - 1;
-    }
-    return lo;
+// Sum over the lanes up to this one.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int add_moved(int v) { return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int scan64(int v) {
+    v = add_moved<0x111, 0xf>(v);      // from 1, 2, 4, 8 lanes before, within 16
+    v = add_moved<0x112, 0xf>(v);
+    v = add_moved<0x114, 0xf>(v);
+    v = add_moved<0x118, 0xf>(v);
+    v = add_moved<0x142, 0xa>(v);      // the last lane of 16 into the next 16, of 32 into the next 32
+    return add_moved<0x143, 0xc>(v);
 }
+
+// The tensors of a launch.  A chunk's tensor is the last one whose first chunk is not behind it (tensors without elements have no
+// chunks).  Steps of a search through memory took longer than the chunk itself (150 tensors of 37 MB together: 11.6 us for their
+// squares), so every wavefront holds the list's first chunks in registers, and every workgroup the table's in LDS.
+template <bool TABLE>
+struct Tensors {
+    static constexpr int PER_LANE = (GRAD_LIST + 63) / 64;
+    const GradList& l;
+    const GradTable& table;
+    int n;
+    int own[PER_LANE];      // list: lane i has the first chunks of tensors i, i + 64, ... (behind the last tensor: never reached)
+    int stride;             // table: every stride-th tensor's in LDS
+    const int* lds;
+    __device__ Tensors(const GradList& l, const GradTable& table, int n, int* lds) : l(l), table(table), n(n), stride(1), lds(lds) {
+        if constexpr (TABLE) {
+            stride = (n + GRAD_FIRSTS - 1) / GRAD_FIRSTS;
+            for (int k = threadIdx.x; k * stride < n; k += 256) lds[k] = table.first[k * stride];
+            __syncthreads();
+        } else {
+            int before = 0;
+#pragma unroll
+            for (int b = 0; b < PER_LANE; ++b) {
+                own[b] = INT_MAX;
+                if (b * 64 < n) {
+                    const int k = b * 64 + (threadIdx.x & 63), chunks = k < n ? l.t[k].chunks() : 0, v = before + scan64(chunks);
+                    if (k < n) own[b] = v - chunks;
+                    before = __builtin_amdgcn_readlane(v, 63);
+                }
+            }
+        }
+    }
+    // also the number of the chunk within its tensor
+    __device__ GradTensor of(int c, int& within) const {
+        int k, f = 0;
+        if constexpr (TABLE) {
+            k = search(lds, 0, (n - 1) / stride, c);
+            f = lds[k];
+            if (stride > 1) {
+                const int end = (k + 1) * stride < n ? (k + 1) * stride : n;
+                k = search(table.first, k * stride, end - 1, c);
+                f = table.first[k];
+            }
+            k = __builtin_amdgcn_readfirstlane(k);
+            within = __builtin_amdgcn_readfirstlane(c - f);
+            return table.t[k];
+        } else {
+            k = -1;
+#pragma unroll
+            for (int b = 0; b < PER_LANE; ++b)
+                if (b * 64 < n) {
+                    const int m = __popcll(__ballot(own[b] <= c));
+                    if (m) f = __builtin_amdgcn_readlane(own[b], m - 1);
+                    k += m;
+                }
+            within = c - f;
+            return l.t[k];
+        }
+    }
+    __device__ static int search(const int* first, int lo, int hi, int c) {
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (first[mid] <= c) lo = mid; else hi = mid - 1;
+        }
+        return lo;
+    }
+};
 
 __device__ __forceinline__ float bf16_to_f32(unsigned short b) { return __uint_as_float((unsigned)b << 16); }
 __device__ __forceinline__ unsigned short f32_to_bf16(float v) {
@@ -76,12 +159,13 @@ __device__ __forceinline__ void add_squares(double* s, u16x8u v) {
     }
 }
 
-// Squares of one chunk: elements [e0, e1) of a tensor.
+// Squares of a tensor's chunk.
 template <typename V, typename T>
-__device__ __forceinline__ void chunk_squares(const T* g, int64_t e0, int64_t e1, double* s) {
-    constexpr int E = 16 / sizeof(T), STEPS = GRAD_CHUNK_BYTES / 16 / 256;
-    const T* p = g + e0 + threadIdx.x * E;
-    if (e1 - e0 == GRAD_CHUNK_BYTES / (int)sizeof(T)) {
+__device__ __forceinline__ void chunk_squares(const T* g, int64_t count, int within, double* s) {
+    constexpr int E = 16 / sizeof(T), CHUNK = GRAD_CHUNK_BYTES / sizeof(T), STEPS = CHUNK / (256 * E);
+    const int64_t e0 = (int64_t)within * CHUNK, left = count - e0;
+    const T* p = global(g) + e0 + threadIdx.x * E;
+    if (left >= CHUNK) {
         V v[STEPS];
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) v[i] = *reinterpret_cast<const V*>(p + i * 256 * E);
@@ -89,7 +173,7 @@ __device__ __forceinline__ void chunk_squares(const T* g, int64_t e0, int64_t e1
         for (int i = 0; i < STEPS; ++i) add_squares(s, v[i]);
         return;
     }
-    const int n = (int)(e1 - e0);
+    const int n = (int)left;
     for (int j = threadIdx.x * E; j < n; j += 256 * E, p += 256 * E) {
         if (j + E <= n) {
             add_squares(s, *reinterpret_cast<const V*>(p));
@@ -111,20 +195,25 @@ __device__ __forceinline__ u16x8u times(u16x8u v, float f) {
 __device__ __forceinline__ float times1(float v, float f) { return v * f; }
 __device__ __forceinline__ unsigned short times1(unsigned short v, float f) { return f32_to_bf16(bf16_to_f32(v) * f); }
 
-template <typename V, typename T>
-__device__ __forceinline__ void chunk_scale(const T* g, T* o, int64_t e0, int64_t e1, float f) {
-    constexpr int E = 16 / sizeof(T), STEPS = GRAD_CHUNK_BYTES / 16 / 256;
-    const T* p = g + e0 + threadIdx.x * E;
-    T* q = o + e0 + threadIdx.x * E;
-    if (e1 - e0 == GRAD_CHUNK_BYTES / (int)sizeof(T)) {
+template <bool STREAM, typename V, typename T>
+__device__ __forceinline__ void chunk_scale(const T* g, T* o, int64_t count, int within, float f) {
+    constexpr int E = 16 / sizeof(T), CHUNK = GRAD_CHUNK_BYTES / sizeof(T), STEPS = CHUNK / (256 * E);
+    const int64_t e0 = (int64_t)within * CHUNK, left = count - e0;
+    const T* p = global(g) + e0 + threadIdx.x * E;
+    T* q = global(o) + e0 + threadIdx.x * E;
+    if (left >= CHUNK) {
         V v[STEPS];
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) v[i] = *reinterpret_cast<const V*>(p + i * 256 * E);
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) *reinterpret_cast<V*>(q + i * 256 * E) = times(v[i], f);
+        for (int i = 0; i < STEPS; ++i) {
+            V* at = reinterpret_cast<V*>(q + i * 256 * E);
+            if constexpr (STREAM) __builtin_nontemporal_store(times(v[i], f), at);
+            else *at = times(v[i], f);
+        }
         return;
     }
-    const int n = (int)(e1 - e0);
+    const int n = (int)left;
     for (int j = threadIdx.x * E; j < n; j += 256 * E, p += 256 * E, q += 256 * E) {
         if (j + E <= n) {
             *reinterpret_cast<V*>(q) = times(*reinterpret_cast<const V*>(p), f);
@@ -134,8 +223,16 @@ __device__ __forceinline__ void chunk_scale(const T* g, T* o, int64_t e0, int64_
     }
 }
 
-__global__ __launch_bounds__(128) void grad_table_kernel(GradList l, GradTensor* table) {
-    for (int i = threadIdx.x; i < l.n; i += 128) table[l.at + i] = l.t[i];
+__global__ __launch_bounds__(64) void grad_table_kernel(GradList l, GradTable table) {
+    int before = l.first;
+    for (int k0 = 0; k0 < l.n; k0 += 64) {
+        const int k = k0 + threadIdx.x, chunks = k < l.n ? l.t[k].chunks() : 0, v = before + scan64(chunks);
+        if (k < l.n) {
+            table.t[l.at + k] = l.t[k];
+            table.first[l.at + k] = v - chunks;
+        }
+        before = __builtin_amdgcn_readlane(v, 63);
+    }
 }
 
 // Sum of the partial sums in a fixed order (all 256 threads get it).
@@ -145,22 +242,18 @@ __device__ __forceinline__ float norm_of(const double* part, int parts, double* 
     return (float)sqrt(block_sum64(s, sh));
 }
 
-// part[b]: workgroup b's sum of squares.  A single workgroup writes the norm itself.
+// part[b]: workgroup b's sum of squares.  A single workgroup writes the norm itself, where that is what is asked for.
 template <bool TABLE>
-__global__ __launch_bounds__(256) void grad_squares_kernel(GradList l, const GradTensor* table, int n, int chunks, double* part,
-                                                           float* norm) {
+__global__ __launch_bounds__(256) void grad_squares_kernel(GradList l, GradTable table, int n, int chunks, double* part, float* norm) {
     __shared__ double sh[4];
-    const GradTensor* ts = TABLE ? table : l.t;
+    __shared__ int firsts[TABLE ? GRAD_FIRSTS : 1];
+    const Tensors<TABLE> ts(l, table, n, firsts);
     double s[2] = {0.0, 0.0};
     for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
-        const GradTensor t = ts[tensor_of(ts, n, c)];
-        if (t.bf16) {
-            const int64_t e0 = (int64_t)(c - t.first) * (GRAD_CHUNK_BYTES / 2), e1 = e0 + GRAD_CHUNK_BYTES / 2;
-            chunk_squares<u16x8u>((const u16*)t.g, e0, e1 < t.count ? e1 : t.count, s);
-        } else {
-            const int64_t e0 = (int64_t)(c - t.first) * (GRAD_CHUNK_BYTES / 4), e1 = e0 + GRAD_CHUNK_BYTES / 4;
-            chunk_squares<f32x4u>((const float*)t.g, e0, e1 < t.count ? e1 : t.count, s);
-        }
+        int within;
+        const GradTensor t = ts.of(c, within);
+        if (t.bf16()) chunk_squares<u16x8u>((const u16*)t.g, t.count(), within, s);
+        else chunk_squares<f32x4u>((const float*)t.g, t.count(), within, s);
     }
     const double sum = block_sum64(s[0] + s[1], sh);
     if (threadIdx.x == 0) {
@@ -177,12 +270,13 @@ __global__ __launch_bounds__(256) void grad_norm_kernel(const double* part, int 
 
 // parts > 0: the norm comes from the partial sums (every workgroup folds them, which spares a launch) and is written by
 // workgroup 0; else it is read.  The chunks are taken from the last to the first: what the norm's launch read last is still in
-// the 256 MB infinity cache.
-template <bool TABLE>
-__global__ __launch_bounds__(256) void grad_scale_kernel(GradList l, const GradTensor* table, int n, int chunks, int in_place,
+// the 256 MB infinity cache.  STREAM: what is written does not go there (it would only push out what is still to be read; eight
+// shards of 4000 x 4096 into other tensors: 300 -> 273 us).
+template <bool TABLE, bool STREAM>
+__global__ __launch_bounds__(256) void grad_scale_kernel(GradList l, GradTable table, int n, int chunks, int in_place,
                                                          const double* part, int parts, float max_norm, float* norm) {
     __shared__ double sh[4];
-    const GradTensor* ts = TABLE ? table : l.t;
+    __shared__ int firsts[TABLE ? GRAD_FIRSTS : 1];
     float v;
     if (parts) {
         v = norm_of(part, parts, sh);
@@ -192,41 +286,45 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(GradList l, const GradT
     }
     const float f = v > max_norm && v < INFINITY ? max_norm / v : 1.f;
     if (f == 1.f && in_place) return;
+    const Tensors<TABLE> ts(l, table, n, firsts);
     for (int c = chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
-        const GradTensor t = ts[tensor_of(ts, n, c)];
-        if (t.bf16) {
-            const int64_t e0 = (int64_t)(c - t.first) * (GRAD_CHUNK_BYTES / 2), e1 = e0 + GRAD_CHUNK_BYTES / 2;
-            chunk_scale<u16x8u>((const u16*)t.g, (u16*)t.o, e0, e1 < t.count ? e1 : t.count, f);
-        } else {
-            const int64_t e0 = (int64_t)(c - t.first) * (GRAD_CHUNK_BYTES / 4), e1 = e0 + GRAD_CHUNK_BYTES / 4;
-            chunk_scale<f32x4u>((const float*)t.g, (float*)t.o, e0, e1 < t.count ? e1 : t.count, f);
-        }
+        int within;
+        const GradTensor t = ts.of(c, within);
+        if (t.bf16()) chunk_scale<STREAM, u16x8u>((const u16*)t.g, (u16*)t.o, t.count(), within, f);
+        else chunk_scale<STREAM, f32x4u>((const float*)t.g, (float*)t.o, t.count(), within, f);
     }
 }
 
-}  // namespace
+struct GradCall {
+    const void* const* grads;
+    const int64_t* counts;
+    const int32_t* dts;
+    int32_t n;
+    void* const* outs;
+    float max_norm;
+    bool known;
+    float* norm;
+    double* part;
+    GradTable table;
+    hipStream_t st;
+};
 
-size_t grad_workspace(int32_t n) {
-    return GRAD_BLOCKS * sizeof(double) + (n > GRAD_LIST ? align_up((size_t)n * sizeof(GradTensor), 256) : 0);
-}
-
-hipError_t launch_grad(const void* const* grads, const int64_t* counts, const int32_t* dts, int32_t n, void* const* outs,
-                       float max_norm, bool known, float* norm, void* workspace, hipStream_t st) {
-    double* part = (double*)workspace;
-    GradTensor* table = (GradTensor*)(part + GRAD_BLOCKS);
-    const bool in_table = n > GRAD_LIST;
+template <bool TABLE, bool STREAM>
+hipError_t launch_grad_call(const GradCall& a) {
     GradList l;
-    l.n = l.at = 0;
+    l.n = l.at = l.first = 0;
     int64_t chunks = 0;
     {
-        ProfScope prof(known ? K_GRAD_SCALE : K_GRAD_NORM, st);
-        for (int32_t k = 0; k < n; ++k) {
-            const int bf16 = dts[k] == VP_BF16;
-            l.t[l.n++] = GradTensor{grads[k], outs ? outs[k] : const_cast<void*>(grads[k]), counts[k], (int)chunks, bf16};
-            chunks += ceil_div(counts[k] * (bf16 ? 2 : 4), GRAD_CHUNK_BYTES);
-            if (in_table && (l.n == GRAD_LIST || k == n - 1)) {
-                hipLaunchKernelGGL(grad_table_kernel, dim3(1), dim3(128), 0, st, l, table);
+        ProfScope prof(a.known ? K_GRAD_SCALE : K_GRAD_NORM, a.st);
+        for (int32_t k = 0; k < a.n; ++k) {
+            const GradTensor t{a.grads[k], a.outs ? a.outs[k] : const_cast<void*>(a.grads[k]),
+                               (uint64_t)a.counts[k] * 2 + (a.dts[k] == VP_BF16 ? 1 : 0)};
+            l.t[l.n++] = t;
+            chunks += t.chunks();
+            if (TABLE && (l.n == GRAD_LIST || k == a.n - 1)) {
+                hipLaunchKernelGGL(grad_table_kernel, dim3(1), dim3(64), 0, a.st, l, a.table);
                 l.at = k + 1;
+                l.first = (int)chunks;
                 l.n = 0;
             }
         }
@@ -234,24 +332,37 @@ hipError_t launch_grad(const void* const* grads, const int64_t* counts, const in
         if (e != hipSuccess) return e;
     }
     const int blocks = chunks < 1 ? 1 : chunks < GRAD_BLOCKS ? (int)chunks : GRAD_BLOCKS;
-    if (!known) {
-        ProfScope prof(K_GRAD_NORM, st);
-        const bool alone = max_norm < 0.f;
-        if (in_table)
-            hipLaunchKernelGGL(grad_squares_kernel<true>, dim3(blocks), dim3(256), 0, st, l, table, n, (int)chunks, part, alone ? norm : nullptr);
-        else
-            hipLaunchKernelGGL(grad_squares_kernel<false>, dim3(blocks), dim3(256), 0, st, l, table, n, (int)chunks, part, alone ? norm : nullptr);
-        if (alone && blocks > 1) hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(256), 0, st, part, blocks, norm);
+    if (!a.known) {
+        ProfScope prof(K_GRAD_NORM, a.st);
+        const bool alone = a.max_norm < 0.f;
+        hipLaunchKernelGGL((grad_squares_kernel<TABLE>), dim3(blocks), dim3(256), 0, a.st, l, a.table, a.n, (int)chunks, a.part,
+                           alone ? a.norm : nullptr);
+        if (alone && blocks > 1) hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(256), 0, a.st, a.part, blocks, a.norm);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess || alone) return e;
     }
-    ProfScope prof(K_GRAD_SCALE, st);
-    const int parts = known ? 0 : blocks, in_place = outs == nullptr;
-    if (in_table)
-        hipLaunchKernelGGL(grad_scale_kernel<true>, dim3(blocks), dim3(256), 0, st, l, table, n, (int)chunks, in_place, part, parts, max_norm, norm);
-    else
-        hipLaunchKernelGGL(grad_scale_kernel<false>, dim3(blocks), dim3(256), 0, st, l, table, n, (int)chunks, in_place, part, parts, max_norm, norm);
+    ProfScope prof(K_GRAD_SCALE, a.st);
+    hipLaunchKernelGGL((grad_scale_kernel<TABLE, STREAM>), dim3(blocks), dim3(256), 0, a.st, l, a.table, a.n, (int)chunks,
+                       a.outs == nullptr, a.part, a.known ? 0 : blocks, a.max_norm, a.norm);
     return hipGetLastError();
+}
+
+}  // namespace
+
+size_t grad_workspace(int32_t n) {
+    return GRAD_BLOCKS * sizeof(double) + (n > GRAD_LIST ? align_up((size_t)n * (sizeof(GradTensor) + sizeof(int)), 256) : 0);
+}
+
+hipError_t launch_grad(const void* const* grads, const int64_t* counts, const int32_t* dts, int32_t n, void* const* outs,
+                       float max_norm, bool known, float* norm, void* workspace, hipStream_t st) {
+    int64_t bytes = 0;
+    for (int32_t k = 0; k < n; ++k) bytes += counts[k] * (dts[k] == VP_BF16 ? 2 : 4);
+    double* part = (double*)workspace;
+    GradTensor* table = (GradTensor*)(part + GRAD_BLOCKS);
+    const GradCall a{grads, counts, dts, n, outs, max_norm, known, norm, part, GradTable{table, (int*)(table + n)}, st};
+    const bool stream = bytes > (int64_t)128 << 20;
+    if (n > GRAD_LIST) return stream ? launch_grad_call<true, true>(a) : launch_grad_call<true, false>(a);
+    return stream ? launch_grad_call<false, true>(a) : launch_grad_call<false, false>(a);
 }
 
 }  // namespace vp
