@@ -37,6 +37,7 @@ VP_CALL_OUTPUT_DX_ALG2 = 6
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
 _HOST = None      # _vphost.so, loaded with the library, or None
+_ADDRESS = {}     # of the library's functions that _vphost.so calls itself
 
 
 class VPError(RuntimeError):
@@ -160,6 +161,8 @@ def load_library() -> ctypes.CDLL:
     lib.vp_profile_enable.argtypes = [c.c_int]
     lib.vp_profile_read.restype = c.c_int
     lib.vp_profile_read.argtypes = [c.POINTER(c.c_double), c.POINTER(c.c_int64), c.c_int]
+    for name in ("vp_block_norm_fwd", "vp_block_norm_bwd"):
+        _ADDRESS[name] = c.cast(getattr(lib, name), vp).value
     _LIB = lib
     return lib
 
@@ -559,6 +562,13 @@ def vp_block_norm_fwd(x, y, H, *, r=None, stats=None, gate=None, w=None, b=None,
                       eps: float = 1e-5, post: bool = False, center: bool = False, stream=None) -> None:
     """The norms around a block: u = norm(y) (post) or y, r = x + scale * gate * u, H = norm(r); RMS norms, or layer norms with
     center=True.  y=None: H = norm(x) alone.  r, stats ([4, N], for the backward call) and every vector may be None."""
+    if isinstance(stream, torch.cuda.Stream):
+        stream = stream.cuda_stream
+    if _HOST is not None:
+        st = _HOST.block_norm_fwd(_ADDRESS["vp_block_norm_fwd"], x, y, H, r, stats, gate, w, b, w_post, b_post, scale, eps,
+                                  _norm_flags(post, center), stream)
+        if st == 0:
+            return
     if x.dim() != 2:
         raise VPError("x must be [N, h]")
     N, h = x.shape
@@ -586,6 +596,13 @@ def vp_block_norm_bwd(dH, r, y, stats, *, dx, dy=None, dr=None, gate=None, w=Non
                       workspace=None, stream=None) -> None:
     """The gradients of vp_block_norm_fwd, from its r (x where y was None) and stats.  dH is fp32 or of the type of r; dr, dx
     and dy are of one type, fp32 or that of r; the parameters' gradients are fp32, and None where they are not wanted."""
+    if isinstance(stream, torch.cuda.Stream):
+        stream = stream.cuda_stream
+    if _HOST is not None:
+        st = _HOST.block_norm_bwd(_ADDRESS["vp_block_norm_bwd"], dH, r, y, stats, dx, dy, dr, gate, w, w_post, b_post, scale,
+                                  _norm_flags(post, center), dgate, dw, db, dw_post, db_post, workspace, stream)
+        if st == 0:
+            return
     if r.dim() != 2:
         raise VPError("r must be [N, h]")
     N, h = r.shape
@@ -621,7 +638,9 @@ class GradientArguments:
         self.out_ptrs = None
         if outs is not None:
             self.out_ptrs = (ctypes.c_void_p * n)(*[_ptr(o, "outs", (g.dtype,), g.shape) for g, o in zip(self.grads, self.outs)])
-        self.devices = {t.get_device() for t in self.grads + (self.outs or [])}
+        if len({t.get_device() for t in self.grads + (self.outs or [])}) > 1:
+            raise VPError("gradients of one call are on one device")
+        self.first = self.grads[0] if n else None
         # What is written is written by no order: outputs are apart from one another and from all gradients but their own.
         written = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), k)
                          for k, t in enumerate(self.grads if outs is None else self.outs) if t.numel())
@@ -638,14 +657,18 @@ class GradientArguments:
                         self.overlap = True
 
 
-def _grad_call(name: str, a, written: bool, call, norm, workspace, stream):
-    if written and a.overlap:
+def _grad_call(name: str, a, norm, workspace, stream, max_norm=None):
+    if max_norm is not None and a.overlap:
         raise VPError("%s: an output shares memory with another one or with another gradient" % name)
-    if a.devices - {torch.cuda.current_device()}:
-        raise VPError("%s: gradients on another device than the current one" % name)
-    _on_current_device((norm, workspace))
+    lib = load_library()
+    _on_current_device((a.first, norm, workspace))
     wp, wb = _ws(workspace)
-    _check(call(load_library(), _ptr(norm, "norm", (torch.float32,), (1,)), wp, wb, _stream(stream)), name)
+    np, s = _ptr(norm, "norm", (torch.float32,), (1,)), _stream(stream)
+    if max_norm is None:
+        st = lib.vp_grad_norm(a.ptrs, a.counts, a.dts, a.n, np, wp, wb, s)
+    else:
+        st = getattr(lib, name)(a.ptrs, a.counts, a.dts, a.n, a.out_ptrs, max_norm, np, wp, wb, s)
+    _check(st, name)
 
 
 def _gradients(grads, outs=None) -> GradientArguments:
@@ -665,24 +688,18 @@ def vp_grad_workspace_bytes(n: int) -> int:
 
 def vp_grad_norm(grads, norm, workspace, stream=None) -> None:
     """norm[0] = the 2-norm of all gradients together.  grads: tensors of fp32 or bf16, or GradientArguments made of them once."""
-    a = _gradients(grads)
-    _grad_call("vp_grad_norm", a, False, lambda lib, np, wp, wb, st: lib.vp_grad_norm(
-        a.ptrs, a.counts, a.dts, a.n, np, wp, wb, st), norm, workspace, stream)
+    _grad_call("vp_grad_norm", _gradients(grads), norm, workspace, stream)
 
 
 def vp_grad_clip(grads, max_norm: float, norm, workspace, outs=None, stream=None) -> None:
     """vp_grad_norm, and every gradient times max_norm / norm where the norm exceeds max_norm: in place, or into outs.  A norm
     that is not finite leaves the gradients as they are."""
-    a = _gradients(grads, outs)
-    _grad_call("vp_grad_clip", a, True, lambda lib, np, wp, wb, st: lib.vp_grad_clip(
-        a.ptrs, a.counts, a.dts, a.n, a.out_ptrs, max_norm, np, wp, wb, st), norm, workspace, stream)
+    _grad_call("vp_grad_clip", _gradients(grads, outs), norm, workspace, stream, float(max_norm))
 
 
 def vp_grad_scale(grads, max_norm: float, norm, workspace, outs=None, stream=None) -> None:
     """vp_grad_clip with a norm that is known already."""
-    a = _gradients(grads, outs)
-    _grad_call("vp_grad_scale", a, True, lambda lib, np, wp, wb, st: lib.vp_grad_scale(
-        a.ptrs, a.counts, a.dts, a.n, a.out_ptrs, max_norm, np, wp, wb, st), norm, workspace, stream)
+    _grad_call("vp_grad_scale", _gradients(grads, outs), norm, workspace, stream, float(max_norm))
 
 
 def vp_profile_mfma_loop(operands, out, iters: int, blocks: int, stream=None) -> None:

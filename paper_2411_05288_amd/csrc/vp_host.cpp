@@ -16,6 +16,7 @@
 
 #include <cstdint>
 #include <cstring>
+#include <initializer_list>
 
 namespace {
 
@@ -123,7 +124,139 @@ PyObject* stream(PyObject*, PyObject*) {
     }
 }
 
+// ---- whole calls: checks, addresses and the call itself, without a Python call per tensor (a single token through the norms
+// around a block: 6.7 us of host time with them, 4.3 us so).
+
+// Checks the tensors of one call and collects their addresses.
+struct Call {
+    at::DeviceIndex here = c10::hip::current_device();
+    bool ok = true;
+
+    static bool bf16_like(at::ScalarType t) { return t == at::kBFloat16 || t == at::kShort || t == at::kUInt16; }
+    // vp_dtype of a tensor
+    int dtype(PyObject* o) {
+        if (THPVariable_CheckExact(o)) {
+            const at::ScalarType t = THPVariable_Unpack(o).scalar_type();
+            if (t == at::kFloat) return 0;
+            if (bf16_like(t)) return 1;
+        }
+        ok = false;
+        return 0;
+    }
+    // the address of a tensor of the shape and type; None is null
+    void* at(PyObject* o, int dtype, std::initializer_list<int64_t> shape) {
+        if (o == Py_None || !ok) return nullptr;
+        ok = false;
+        if (!THPVariable_CheckExact(o)) return nullptr;
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!t.defined() || !t.is_cuda() || t.get_device() != here || !t.is_contiguous()) return nullptr;
+        if (dtype == 0 ? t.scalar_type() != at::kFloat : !bf16_like(t.scalar_type())) return nullptr;
+        if (t.sizes() != at::IntArrayRef(shape.begin(), shape.size())) return nullptr;
+        ok = true;
+        return t.data_ptr();
+    }
+    // N and h of a matrix; a gate's rows (0 for None)
+    int64_t size(PyObject* o, int64_t d) {
+        if (o == Py_None) return 0;
+        if (!THPVariable_CheckExact(o) || !THPVariable_Unpack(o).defined() || THPVariable_Unpack(o).dim() != 2) {
+            ok = false;
+            return 0;
+        }
+        return THPVariable_Unpack(o).size(d);
+    }
+    // the stream to launch on: the current one for None
+    void* stream(PyObject* o) {
+        if (o == Py_None) return c10::hip::getCurrentHIPStream().stream();
+        if (!PyLong_CheckExact(o)) {
+            ok = false;
+            return nullptr;
+        }
+        return number(PyLong_AsVoidPtr(o));
+    }
+    double real(PyObject* o) { return number(PyFloat_AsDouble(o)); }
+    long integer(PyObject* o) { return number(PyLong_AsLong(o)); }
+    void* pointer(PyObject* o) { return number(PyLong_AsVoidPtr(o)); }
+
+private:
+    template <typename T>
+    T number(T v) {
+        if (PyErr_Occurred()) {
+            PyErr_Clear();
+            ok = false;
+        }
+        return v;
+    }
+};
+
+using Forward = int (*)(const void*, const void*, const void*, int64_t, const void*, const void*, const void*, const void*, int64_t,
+                        int64_t, int, uint32_t, float, float, void*, void*, float*, void*);
+using Backward = int (*)(const void*, int, const void*, const void*, const void*, const void*, int64_t, const void*, const void*,
+                         const void*, const float*, int64_t, int64_t, int, uint32_t, float, int, void*, void*, float*, float*,
+                         float*, float*, float*, void*, size_t, void*);
+
+// block_norm_fwd(function, x, y, H, r, stats, gate, w, b, w_post, b_post, scale, eps, flags, stream) -> status
+PyObject* block_norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 15) Py_RETURN_NONE;
+    int status = 0;
+    try {
+        Call c;
+        const auto f = reinterpret_cast<Forward>(c.pointer(a[0]));
+        const int64_t N = c.size(a[1], 0), h = c.size(a[1], 1), rows = c.size(a[6], 0);
+        if (!c.ok || a[1] == Py_None) Py_RETURN_NONE;
+        const int dt = c.dtype(a[1]);
+        void *x = c.at(a[1], dt, {N, h}), *y = c.at(a[2], dt, {N, h}), *H = c.at(a[3], dt, {N, h}), *r = c.at(a[4], dt, {N, h});
+        void *stats = c.at(a[5], 0, {4, N}), *gate = c.at(a[6], dt, {rows, h}), *w = c.at(a[7], dt, {h}), *b = c.at(a[8], dt, {h});
+        void *w_post = c.at(a[9], dt, {h}), *b_post = c.at(a[10], dt, {h});
+        const float scale = (float)c.real(a[11]), eps = (float)c.real(a[12]);
+        const uint32_t flags = (uint32_t)c.integer(a[13]);
+        void* stream = c.stream(a[14]);
+        if (!c.ok) Py_RETURN_NONE;
+        Py_BEGIN_ALLOW_THREADS
+        status = f(x, y, gate, rows, w_post, b_post, w, b, N, h, dt, flags, scale, eps, r, H, static_cast<float*>(stats), stream);
+        Py_END_ALLOW_THREADS
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    return PyLong_FromLong(status);
+}
+
+// block_norm_bwd(function, dH, r, y, stats, dx, dy, dr, gate, w, w_post, b_post, scale, flags, dgate, dw, db, dw_post, db_post,
+//                workspace, stream) -> status
+PyObject* block_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 21) Py_RETURN_NONE;
+    int status = 0;
+    try {
+        Call c;
+        const auto f = reinterpret_cast<Backward>(c.pointer(a[0]));
+        const int64_t N = c.size(a[2], 0), h = c.size(a[2], 1), rows = c.size(a[8], 0);
+        if (!c.ok || a[2] == Py_None || !THPVariable_CheckExact(a[19])) Py_RETURN_NONE;
+        const int dt = c.dtype(a[2]), dH_dt = c.dtype(a[1]), grad_dt = c.dtype(a[5]);
+        void *dH = c.at(a[1], dH_dt, {N, h}), *r = c.at(a[2], dt, {N, h}), *y = c.at(a[3], dt, {N, h}), *stats = c.at(a[4], 0, {4, N});
+        void *dx = c.at(a[5], grad_dt, {N, h}), *dy = c.at(a[6], grad_dt, {N, h}), *dr = c.at(a[7], grad_dt, {N, h});
+        void *gate = c.at(a[8], dt, {rows, h}), *w = c.at(a[9], dt, {h}), *w_post = c.at(a[10], dt, {h}), *b_post = c.at(a[11], dt, {h});
+        const float scale = (float)c.real(a[12]);
+        const uint32_t flags = (uint32_t)c.integer(a[13]);
+        float *dgate = static_cast<float*>(c.at(a[14], 0, {rows, h})), *dw = static_cast<float*>(c.at(a[15], 0, {h}));
+        float *db = static_cast<float*>(c.at(a[16], 0, {h})), *dw_post = static_cast<float*>(c.at(a[17], 0, {h}));
+        float* db_post = static_cast<float*>(c.at(a[18], 0, {h}));
+        const at::Tensor& ws = THPVariable_Unpack(a[19]);
+        if (!c.ok || !ws.defined() || !ws.is_cuda() || ws.get_device() != c.here || !ws.is_contiguous()) Py_RETURN_NONE;
+        void *workspace = ws.data_ptr(), *stream = c.stream(a[20]);
+        const size_t bytes = ws.nbytes();
+        if (!c.ok) Py_RETURN_NONE;
+        Py_BEGIN_ALLOW_THREADS
+        status = f(dH, dH_dt, dr, r, y, gate, rows, w_post, b_post, w, static_cast<const float*>(stats), N, h, dt, flags, scale,
+                   grad_dt, dx, dy, dgate, dw_post, db_post, dw, db, workspace, bytes, stream);
+        Py_END_ALLOW_THREADS
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    return PyLong_FromLong(status);
+}
+
 PyMethodDef methods[] = {
+    {"block_norm_fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(block_norm_fwd)), METH_FASTCALL, nullptr},
+    {"block_norm_bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(block_norm_bwd)), METH_FASTCALL, nullptr},
     {"ptr", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(ptr)), METH_FASTCALL, nullptr},
     {"ptrs", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(ptrs)), METH_FASTCALL, nullptr},
     {"same_shapes", same_shapes, METH_O, nullptr},

@@ -256,3 +256,59 @@ def test_gradients_that_are_not_wanted():
         results.append(out)
         for k in out:
             assert torch.equal(out[k], results[0][k]), (names, k)
+
+
+def test_wrong_tensors_are_refused_and_launch_nothing(monkeypatch):
+    """The same by the native checks and by those in Python."""
+    import paper_2411_05288_amd as vp
+    import paper_2411_05288_amd.binding as B
+    N, h = 6, 64
+    s = inputs(N, h, BF16, True, 3, True, 1)
+    wide = torch.zeros(N, 2 * h, dtype=BF16, device="cuda")
+    stats, ws = torch.ones(4, N, device="cuda"), torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    f = torch.float32
+    good = dict(x=s["x"], y=s["y"], H=torch.full_like(s["x"], 7.0), r=torch.full_like(s["x"], 7.0), stats=stats, gate=s["gate"], w=s["w"],
+                b=s["b"], w_post=s["w_post"], b_post=s["b_post"], post=True)
+    bad = [dict(x=s["x"].half()), dict(x=wide[:, :h]), dict(x=s["x"].cpu()), dict(x=s["x"][0]), dict(y=s["y"][:5]), dict(y=s["y"].float()),
+           dict(y=wide[:, ::2]), dict(H=None), dict(H=good["H"].float()), dict(H=good["H"].cpu()), dict(r=wide), dict(stats=stats[:3]),
+           dict(stats=stats.double()), dict(gate=s["gate"][0]), dict(gate=s["gate"][:, :32]), dict(gate=torch.zeros(4, h, dtype=BF16, device="cuda")),
+           dict(w=s["w"].float()), dict(w=s["w"][:63]), dict(b=s["b"].cpu()), dict(w_post=s["w_post"][None]), dict(b_post=wide[0, ::2]),
+           dict(post=False), dict(eps=0.0), dict(eps=float("nan")), dict(scale=float("inf")), dict(y=None), dict(x=wide.view(-1)[1:1 + N * h].view(N, h))]
+    back = dict(dH=torch.zeros(N, h, device="cuda"), r=s["x"], y=s["y"], stats=stats, dx=torch.full((N, h), 7.0, device="cuda"),
+                dy=torch.full((N, h), 7.0, device="cuda"), gate=s["gate"], w=s["w"], w_post=s["w_post"], b_post=s["b_post"], post=True,
+                dw=torch.full((h,), 7.0, device="cuda"), workspace=ws)
+    worse = [dict(dH=back["dH"][:5]), dict(dH=back["dH"].double()), dict(dH=back["dH"].cpu()), dict(r=wide), dict(dx=back["dx"].half()), dict(dy=None),
+             dict(dx=back["dx"].bfloat16()), dict(dr=torch.zeros(N, h, dtype=BF16, device="cuda")), dict(dw=back["dw"].bfloat16()),
+             dict(db=torch.zeros(63, device="cuda")), dict(dgate=torch.zeros(2, h, device="cuda")), dict(dgate=torch.zeros(h, device="cuda")),
+             dict(workspace=None), dict(workspace=ws[:64]), dict(workspace=ws.cpu()), dict(workspace=ws[8:]), dict(stats=None), dict(post=False),
+             dict(y=None), dict(gate=None, dgate=torch.zeros(3, h, device="cuda"))]
+    B.load_library()
+    for host in (B._HOST, None):
+        monkeypatch.setattr(B, "_HOST", host)
+        for wrong in bad:
+            with pytest.raises(vp.VPError):
+                vp.vp_block_norm_fwd(**{**good, **wrong})
+        for wrong in worse:
+            with pytest.raises(vp.VPError):
+                vp.vp_block_norm_bwd(**{**back, **wrong})
+        torch.cuda.synchronize()
+        for t in (good["H"], good["r"], back["dx"], back["dy"], back["dw"]):
+            assert bool((t == 7).all())
+        assert bool((stats == 1).all())
+        # both ways give the same
+        out = [torch.empty_like(s["x"]), torch.empty_like(s["x"]), torch.empty_like(stats)]
+        vp.vp_block_norm_fwd(**{**good, "H": out[0], "r": out[1], "stats": out[2]})
+        if host is not None:
+            first = out
+        assert all(torch.equal(a, b) for a, b in zip(out, first))
+    with pytest.raises(TypeError):
+        vp.vp_grad_clip([back["dx"]], None, back["dw"][:1], ws)
+
+
+def test_bf16_as_bit_patterns():
+    import paper_2411_05288_amd as vp
+    s = inputs(5, 200, BF16, False, 0, False, 6)
+    a, b = torch.empty_like(s["x"]), torch.empty_like(s["x"])
+    vp.vp_block_norm_fwd(s["x"], None, a, w=s["w"])
+    vp.vp_block_norm_fwd(s["x"].view(torch.int16), None, b, w=s["w"])
+    assert torch.equal(a, b)
