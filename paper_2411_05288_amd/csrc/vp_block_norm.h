@@ -25,6 +25,8 @@ struct Raw8<u16> {
     u16x8u v;
     __device__ float operator[](int e) const { return __uint_as_float((unsigned)v[e] << 16); }
     __device__ void load(const u16* p) { v = *reinterpret_cast<const u16x8u*>(p); }
+    // past the caches: for what is not read again
+    __device__ void load_last(const u16* p) { v = __builtin_nontemporal_load(reinterpret_cast<const u16x8u*>(p)); }
     __device__ void store(u16* p) const { *reinterpret_cast<u16x8u*>(p) = v; }
     __device__ void set(int e, float f) {
         const __bf16 b = (__bf16)f;
@@ -41,6 +43,7 @@ struct Raw8<float> {
         a = *reinterpret_cast<const f32x4u*>(p);
         b = *reinterpret_cast<const f32x4u*>(p + 4);
     }
+    __device__ void load_last(const float* p) { load(p); }      // (two vectors share a line)
     __device__ void store(float* p) const {
         *reinterpret_cast<f32x4u*>(p) = a;
         *reinterpret_cast<f32x4u*>(p + 4) = b;
@@ -49,11 +52,12 @@ struct Raw8<float> {
     __device__ void keep() { asm volatile("" : "+v"(a), "+v"(b)); }
 };
 // Columns j .. j + 7 (`absent` eight times where p is NULL).
-template <typename T>
+template <bool LAST = false, typename T>
 __device__ __forceinline__ Raw8<T> load8(const T* p, int j, float absent = 0.f) {
     Raw8<T> o;
     if (p) {
-        o.load(p + j);
+        if constexpr (LAST) o.load_last(p + j);
+        else o.load(p + j);
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) o.set(e, absent);
@@ -332,13 +336,16 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(BlockNormGrad p, C
                 if (live) add(K::DWP, c, fresh, o);
             }
         }
+        // nothing of the row itself is needed from here on: the next row's values come while this one's second sums are formed
+        const float rho1 = v.rho1;
+        if (it + 1 < s.each) v = load(i + s.step);
         if constexpr (POST) {
             row_sums<M, SMALL>(more, sh, turn, group * waves, waves);
             const float mky = more[0] * inv_h, mk = FULL && p.center ? more[1] * inv_h : 0.f;
 #pragma unroll
             for (int c = 0; c < C; ++c)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) g[c][e] = v.rho1 * ((FULL ? g[c][e] - mk : g[c][e]) - rh[c][e] * mky);
+                for (int e = 0; e < 8; ++e) g[c][e] = rho1 * ((FULL ? g[c][e] - mk : g[c][e]) - rh[c][e] * mky);
         }
 #pragma unroll
         for (int c = 0; c < C; ++c)
@@ -363,7 +370,6 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(BlockNormGrad p, C
                 store8(o, j[c], skip[c], q);
             }
         }
-        if (it + 1 < s.each) v = load(i + s.step);
     }
     // What the groups of the workgroup have summed, added up in order in LDS.  (Kinds in registers come last: they take a slot.)
 #pragma unroll

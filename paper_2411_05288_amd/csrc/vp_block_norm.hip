@@ -86,7 +86,7 @@ __global__ __launch_bounds__(1024) void block_norm_fwd_long_kernel(BlockNorm p) 
 
 // Rows of at most 8 C TR columns: TR lanes (TR <= 64) or the workgroup's up to TR threads hold a row in registers, C vectors of
 // eight columns each, from the only read of x and y to the only write of r and H.
-template <typename T, int TR, int C>
+template <typename T, int TR, int C, bool STREAM>
 __global__ __launch_bounds__(TR <= 64 ? 256 : TR) void block_norm_fwd_kernel(BlockNorm p) {
     __shared__ float sh[2][K_ROW_SUMS];
     int turn = 0;
@@ -106,8 +106,8 @@ __global__ __launch_bounds__(TR <= 64 ? 256 : TR) void block_norm_fwd_kernel(Blo
         const Columns cols(c * threads + t, p.h);
         j[c] = cols.j;
         skip[c] = cols.skip;
-        rx[c] = load8(x, j[c]);
-        if (y) ry[c] = load8(y + at, j[c]);
+        rx[c] = load8<STREAM>(x, j[c]);
+        if (y) ry[c] = load8<STREAM>(y + at, j[c]);
         if (gate) rg[c] = load8(gate, j[c]);
     }
     auto load_post = [&](int c) {
@@ -369,6 +369,10 @@ ColumnSums cut(int64_t N, int64_t h, int64_t gate_rows) {
     s.each = (int)ceil_div(N, parts * s.rows);
     s.ranges = (int)ceil_div(N, s.each);
     s.parts = (int)ceil_div(s.ranges, s.rows);
+    if (bwd_in_one_pass(h)) {      // few rows: on as many CUs as there are
+        s.rows = (int)ceil_div(s.ranges, CUS);
+        s.parts = (int)ceil_div(s.ranges, s.rows);
+    }
     if (bwd_in_one_pass(h) && (gate_rows <= 1 || gate_rows == N)) s.step = s.ranges = s.parts * s.rows;
     s.pitch = (int)((h + 3) / 4 * 4);
     return s;
@@ -380,12 +384,15 @@ constexpr int MAX_ROW_BLOCKS = 1 << 16;
 
 hipError_t launch_block_norm_fwd(const BlockNorm& p, vp_dtype dt, hipStream_t st) {
     ProfScope prof(K_BLOCK_NORM_FWD, st);
-    const bool bf16 = dt == VP_BF16;
+    // bf16 inputs that the infinity cache cannot have held since they were written are read past the caches: N=4096 h=4096 28.0 -> 26.3
+    // us, h=8192 with an element-wise gate 62.4 -> 59.8; smaller ones may still be there (N=2048 h=4096: 13.5 -> 16.1)
+    const bool bf16 = dt == VP_BF16, stream = bf16 && (int64_t)p.N * p.h * 8 > (int64_t)96 << 20;
 #define VP_FWD(TR, C, THREADS)                                                                                                 \
     do {                                                                                                                       \
         const dim3 grid((unsigned)ceil_div(p.N, TR <= 64 ? 256 / TR : 1)), block(TR <= 64 ? 256 : (THREADS));                   \
-        if (bf16) hipLaunchKernelGGL((block_norm_fwd_kernel<u16, TR, C>), grid, block, 0, st, p);                              \
-        else hipLaunchKernelGGL((block_norm_fwd_kernel<float, TR, C>), grid, block, 0, st, p);                                 \
+        if (stream) hipLaunchKernelGGL((block_norm_fwd_kernel<u16, TR, C, true>), grid, block, 0, st, p);                      \
+        else if (bf16) hipLaunchKernelGGL((block_norm_fwd_kernel<u16, TR, C, false>), grid, block, 0, st, p);                  \
+        else hipLaunchKernelGGL((block_norm_fwd_kernel<float, TR, C, false>), grid, block, 0, st, p);                          \
         return hipGetLastError();                                                                                              \
     } while (0)
     if (p.h >= MIN_COLUMNS) {

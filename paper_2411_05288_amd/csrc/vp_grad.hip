@@ -16,10 +16,10 @@
 namespace vp {
 
 namespace {
-
 constexpr int GRAD_LIST = 160;              // tensors in the kernel arguments
 constexpr int GRAD_CHUNK_BYTES = 32768;     // 256 threads, eight loads of 16 bytes each
 constexpr int GRAD_BLOCKS = 1024;           // partial sums at most
+constexpr int GRAD_KEEP = (192 << 20) / GRAD_CHUNK_BYTES;      // chunks that the infinity cache holds from one launch to the next
 constexpr int GRAD_FIRSTS = 2048;           // numbers of first chunks that a workgroup holds in LDS
 
 struct GradTensor {
@@ -160,7 +160,7 @@ __device__ __forceinline__ void add_squares(double* s, u16x8u v) {
 }
 
 // Squares of a tensor's chunk.
-template <typename V, typename T>
+template <bool KEEP, typename V, typename T>
 __device__ __forceinline__ void chunk_squares(const T* g, int64_t count, int within, double* s) {
     constexpr int E = 16 / sizeof(T), CHUNK = GRAD_CHUNK_BYTES / sizeof(T), STEPS = CHUNK / (256 * E);
     const int64_t e0 = (int64_t)within * CHUNK, left = count - e0;
@@ -168,7 +168,10 @@ __device__ __forceinline__ void chunk_squares(const T* g, int64_t count, int wit
     if (left >= CHUNK) {
         V v[STEPS];
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) v[i] = *reinterpret_cast<const V*>(p + i * 256 * E);
+        for (int i = 0; i < STEPS; ++i) {
+            const V* at = reinterpret_cast<const V*>(p + i * 256 * E);
+            v[i] = KEEP ? *at : __builtin_nontemporal_load(at);
+        }
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) add_squares(s, v[i]);
         return;
@@ -204,7 +207,7 @@ __device__ __forceinline__ void chunk_scale(const T* g, T* o, int64_t count, int
     if (left >= CHUNK) {
         V v[STEPS];
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) v[i] = *reinterpret_cast<const V*>(p + i * 256 * E);
+        for (int i = 0; i < STEPS; ++i) v[i] = __builtin_nontemporal_load(reinterpret_cast<const V*>(p + i * 256 * E));
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
             V* at = reinterpret_cast<V*>(q + i * 256 * E);
@@ -244,7 +247,8 @@ __device__ __forceinline__ float norm_of(const double* part, int parts, double* 
 
 // part[b]: workgroup b's sum of squares.  A single workgroup writes the norm itself, where that is what is asked for.
 template <bool TABLE>
-__global__ __launch_bounds__(256) void grad_squares_kernel(GradList l, GradTable table, int n, int chunks, double* part, float* norm) {
+__global__ __launch_bounds__(256) void grad_squares_kernel(GradList l, GradTable table, int n, int chunks, int keep, double* part,
+                                                           float* norm) {
     __shared__ double sh[4];
     __shared__ int firsts[TABLE ? GRAD_FIRSTS : 1];
     const Tensors<TABLE> ts(l, table, n, firsts);
@@ -252,8 +256,13 @@ __global__ __launch_bounds__(256) void grad_squares_kernel(GradList l, GradTable
     for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
         int within;
         const GradTensor t = ts.of(c, within);
-        if (t.bf16()) chunk_squares<u16x8u>((const u16*)t.g, t.count(), within, s);
-        else chunk_squares<f32x4u>((const float*)t.g, t.count(), within, s);
+        if (c >= keep) {
+            if (t.bf16()) chunk_squares<true, u16x8u>((const u16*)t.g, t.count(), within, s);
+            else chunk_squares<true, f32x4u>((const float*)t.g, t.count(), within, s);
+        } else {
+            if (t.bf16()) chunk_squares<false, u16x8u>((const u16*)t.g, t.count(), within, s);
+            else chunk_squares<false, f32x4u>((const float*)t.g, t.count(), within, s);
+        }
     }
     const double sum = block_sum64(s[0] + s[1], sh);
     if (threadIdx.x == 0) {
@@ -335,8 +344,8 @@ hipError_t launch_grad_call(const GradCall& a) {
     if (!a.known) {
         ProfScope prof(K_GRAD_NORM, a.st);
         const bool alone = a.max_norm < 0.f;
-        hipLaunchKernelGGL((grad_squares_kernel<TABLE>), dim3(blocks), dim3(256), 0, a.st, l, a.table, a.n, (int)chunks, a.part,
-                           alone ? a.norm : nullptr);
+        hipLaunchKernelGGL((grad_squares_kernel<TABLE>), dim3(blocks), dim3(256), 0, a.st, l, a.table, a.n, (int)chunks,
+                           (int)(alone ? chunks : chunks - GRAD_KEEP), a.part, alone ? a.norm : nullptr);
         if (alone && blocks > 1) hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(256), 0, a.st, a.part, blocks, a.norm);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess || alone) return e;
