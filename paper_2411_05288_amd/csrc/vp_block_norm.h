@@ -146,13 +146,14 @@ struct ColumnSums {
 enum : int { NORM_POST = 1, NORM_GATE = 2, NORM_FULL = 4 };      // FULL: layer norms, or db or db_post is wanted
 
 // Where the sums over tokens of a thread's columns are kept: kind 0 is dw, the others are numbered as they are there.  C = 1
-// (up to 8192 columns): two kinds in registers, the others in LDS.  C = 2 (up to 16384): two in LDS, the others in the workgroup's
-// row of the partial matrices, which the L2 holds.
+// (up to 8192 columns): two kinds in registers, the others in LDS.  C = 2 (up to 16384): two in LDS, one in registers, the others
+// in the workgroup's row of the partial matrices, which the L2 holds.
 template <int C, int PARTS>
 struct Kinds {
     static constexpr bool POST = PARTS & NORM_POST, GATE = PARTS & NORM_GATE, FULL = PARTS & NORM_FULL;
     static constexpr int DW = 0, DWP = 1, DG = 1 + POST, DB = 1 + POST + GATE, DBP = DB + 1, COUNT = 1 + POST + GATE + FULL * (1 + POST);
     static constexpr int LDS0 = C == 1 ? 2 : 0, LDS1 = C == 1 ? COUNT : (COUNT < 2 ? COUNT : 2);      // kinds in LDS
+    static constexpr bool in_registers(int kind) { return C == 1 ? kind < 2 : kind == 2; }
     static constexpr int SLOTS = LDS1 > LDS0 ? LDS1 - LDS0 : (C == 1 ? 1 : 0);
 };
 
@@ -182,20 +183,20 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(BlockNormGrad p, C
         j[c] = cols.j;
         skip[c] = cols.skip;
     }
-    float reg[2][8];
+    float reg[2][8];      // of a kind (C = 1), of a vector (C = 2)
+    auto in_reg = [&](int kind, int c) -> float* { return reg[C == 1 ? (kind < 2 ? kind : 0) : c]; };
     auto slot = [&](int kind, int c, int half) -> float4& { return lds[(((kind - K::LDS0) * C + c) * 2 + half) * 1024 + threadIdx.x]; };
     auto matrix = [&](int kind) {
         return kind == K::DW ? s.dw : POST && kind == K::DWP ? s.dw_post : GATE && kind == K::DG ? s.dgate : kind == K::DB ? s.db : s.db_post;
     };
 #pragma unroll
-    for (int k = 0; k < K::COUNT; ++k) {
-        if (k < 2)
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) reg[k][e] = 0.f;
+        for (int e = 0; e < 8; ++e) reg[k][e] = 0.f;
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-            if (k >= K::LDS0 && k < K::LDS1) slot(k, c, 0) = slot(k, c, 1) = make_float4(0.f, 0.f, 0.f, 0.f);
-    }
+    for (int k = K::LDS0; k < K::LDS1; ++k)
+#pragma unroll
+        for (int c = 0; c < C; ++c) slot(k, c, 0) = slot(k, c, 1) = make_float4(0.f, 0.f, 0.f, 0.f);
     // the values of a kind that is not in registers: v, or what is kept with `add` more
     auto kept = [&](int kind, int c, bool fresh, float* v) {
         if (kind < K::LDS1) {
@@ -217,86 +218,113 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(BlockNormGrad p, C
         }
     };
     auto add = [&](int kind, int c, bool fresh, float* v) {
-        if (C == 1 && kind < 2) {
+        if (K::in_registers(kind)) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) reg[kind][e] += v[e];
+            for (int e = 0; e < 8; ++e) in_reg(kind, c)[e] += v[e];
         } else if (kind < K::LDS1 || matrix(kind)) {
             kept(kind, c, fresh, v);
             keep(kind, c, v);
         }
     };
+    // What is read of a row.  C = 1: once, and kept in registers from the first sums to the last.  C = 2: again in every step, from
+    // the caches (two vectors of everything at once do not fit: N=2048 h=16384, kept, 124 us for bf16 RMS norms, 215 for fp32 ones
+    // and 270 with everything; read again, 127, 196 and 257).
     struct Values {
-        Raw8<TD> dH[C];
-        Raw8<TG> dr[C];
-        Raw8<T> r[C], y[C], gate[C];
+        Raw8<TD> dH;
+        Raw8<TG> dr;
+        Raw8<T> r, y, gate;
+    };
+    struct Statistics {
         float m1, rho1, m2, rho2;
     };
-    auto load = [&](int i) {
-        Values v;
+    auto load_statistics = [&](int i) {
+        Statistics q;
+        i = i < p.N ? i : p.N - 1;
+        if constexpr (POST) {
+            q.m1 = p.stats[i];
+            q.rho1 = p.stats[(size_t)p.N + i];
+        }
+        q.m2 = p.stats[2 * (size_t)p.N + i];
+        q.rho2 = p.stats[3 * (size_t)p.N + i];
+        return q;
+    };
+    auto load_first = [&](Values& v, int i, int c) {
+        const size_t at = (size_t)(i < p.N ? i : p.N - 1) * p.h;
+        v.dH = load8((const TD*)p.dH + at, j[c]);
+        v.r = load8((const T*)p.r + at, j[c]);
+    };
+    auto load_second = [&](Values& v, int i, int c) {
         i = i < p.N ? i : p.N - 1;
         const size_t at = (size_t)i * p.h;
-        if constexpr (POST) {
-            v.m1 = p.stats[i];
-            v.rho1 = p.stats[(size_t)p.N + i];
-        }
-        v.m2 = p.stats[2 * (size_t)p.N + i];
-        v.rho2 = p.stats[3 * (size_t)p.N + i];
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            v.dH[c] = load8((const TD*)p.dH + at, j[c]);
-            v.r[c] = load8((const T*)p.r + at, j[c]);
-            v.dr[c] = load8(p.dr ? (const TG*)p.dr + at : nullptr, j[c]);
-            if constexpr (POST || GATE) v.y[c] = load8((const T*)p.y + at, j[c]);
-            if constexpr (GATE) v.gate[c] = load8((const T*)p.gate + (size_t)(i / L) * p.h, j[c]);
-        }
-        return v;
+        v.dr = load8(p.dr ? (const TG*)p.dr + at : nullptr, j[c]);
+        if constexpr (POST || GATE) v.y = load8((const T*)p.y + at, j[c]);
+        if constexpr (GATE) v.gate = load8((const T*)p.gate + (size_t)(i / L) * p.h, j[c]);
     };
-    Raw8<T> w[C], wp[C], bp[C];
-    auto load_vectors = [&]() {
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            w[c] = load8((const T*)p.w, j[c], 1.f);
-            if constexpr (POST) wp[c] = load8((const T*)p.w_post, j[c], 1.f);
-            if constexpr (POST && GATE) bp[c] = load8((const T*)p.b_post, j[c]);
-            // what a skipped column would add to the sums over a row has its weight as a factor
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                w[c].set(e, e < skip[c] ? 0.f : w[c][e]);
-                if constexpr (POST) wp[c].set(e, e < skip[c] ? 0.f : wp[c][e]);
-            }
-        }
+    struct Vectors {
+        Raw8<T> w, wp, bp;
     };
-    Values v = load(i0);
-    if constexpr (C == 1) load_vectors();
+    auto load_vectors = [&](int c) {
+        Vectors q;
+        q.w = load8((const T*)p.w, j[c], 1.f);
+        if constexpr (POST) q.wp = load8((const T*)p.w_post, j[c], 1.f);
+        if constexpr (POST && GATE) q.bp = load8((const T*)p.b_post, j[c]);
+        // what a skipped column would add to the sums over a row has its weight as a factor
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            q.w.set(e, e < skip[c] ? 0.f : q.w[e]);
+            if constexpr (POST) q.wp.set(e, e < skip[c] ? 0.f : q.wp[e]);
+        }
+        return q;
+    };
+    Values v;
+    Vectors q;
+    Statistics u = load_statistics(i0);
+    if constexpr (C == 1) {
+        load_first(v, i0, 0);
+        load_second(v, i0, 0);
+        q = load_vectors(0);
+    }
     for (int it = 0; it < s.each; ++it) {
         const int i = i0 + it * s.step;
         const bool live = i < i1, fresh = it == 0;      // (a workgroup's groups go through the same barriers)
-        if constexpr (C > 1) load_vectors();
-#pragma unroll
-        for (int c = 0; c < C; ++c) {      // (the vectors stay as they are stored: converted ahead of the loop they take twice the registers)
-            w[c].keep();
-            if constexpr (POST) wp[c].keep();
-            if constexpr (POST && GATE) bp[c].keep();
+        // (the vectors stay as they are stored: converted ahead of the loop they take twice the registers)
+        if constexpr (C == 1) {
+            q.w.keep();
+            if constexpr (POST) q.wp.keep();
+            if constexpr (POST && GATE) q.bp.keep();
         }
         const size_t at = (size_t)(live ? i : 0) * p.h;
-        constexpr int M = FULL ? 2 : 1;      // sums over a row: of v rh and, for its mean, of v
-        float rh[C][8], g[C][8], sums[2] = {0.f, 0.f};
+        constexpr int M = FULL ? 2 : 1;      // sums over a row: of a value times rh or yh and, for its mean, of the value
+        float rh[8], g[C][8], sums[2] = {0.f, 0.f};
+        auto first_step = [&](int c) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                rh[e] = (FULL ? v.r[e] - u.m2 : v.r[e]) * u.rho2;
+                g[c][e] = v.dH[e] * q.w[e];
+            }
+        };
+        auto normed_y = [&](const Raw8<T>& y, float m1, float rho1) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) rh[e] = (FULL ? y[e] - m1 : y[e]) * rho1;
+        };
 #pragma unroll
         for (int c = 0; c < C; ++c) {
+            if constexpr (C > 1) {
+                load_first(v, i, c);
+                q = load_vectors(c);
+            }
+            first_step(c);
             float o[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float dH = v.dH[c][e];
-                rh[c][e] = (FULL ? v.r[c][e] - v.m2 : v.r[c][e]) * v.rho2;
-                g[c][e] = dH * w[c][e];
-                o[e] = dH * rh[c][e];
-                sums[0] += g[c][e] * rh[c][e];
+                o[e] = v.dH[e] * rh[e];
+                sums[0] += g[c][e] * rh[e];
                 if constexpr (FULL) sums[1] += g[c][e];
             }
             if (live) add(K::DW, c, fresh, o);
             if constexpr (FULL) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = v.dH[c][e];
+                for (int e = 0; e < 8; ++e) o[e] = v.dH[e];
                 if (live) add(K::DB, c, fresh, o);
             }
         }
@@ -305,21 +333,25 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(BlockNormGrad p, C
         float more[2] = {0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < C; ++c) {
+            if constexpr (C > 1) {
+                load_first(v, i, c);
+                load_second(v, i, c);
+                q = load_vectors(c);
+                first_step(c);
+            }
             float o[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) g[c][e] = v.dr[c][e] + v.rho2 * ((FULL ? g[c][e] - ma : g[c][e]) - rh[c][e] * mar);
+            for (int e = 0; e < 8; ++e) g[c][e] = v.dr[e] + u.rho2 * ((FULL ? g[c][e] - ma : g[c][e]) - rh[e] * mar);
             if (live) store8((TG*)p.dx + at, j[c], skip[c], g[c]);
-            if constexpr (POST)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) rh[c][e] = (FULL ? v.y[c][e] - v.m1 : v.y[c][e]) * v.rho1;      // from here on yh
+            if constexpr (POST) normed_y(v.y, u.m1, u.rho1);      // from here on, rh is yh
             if constexpr (GATE) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = p.scale * (POST ? rh[c][e] * wp[c][e] + bp[c][e] : v.y[c][e]) * g[c][e];
+                for (int e = 0; e < 8; ++e) o[e] = p.scale * (POST ? rh[e] * q.wp[e] + q.bp[e] : v.y[e]) * g[c][e];
                 // (sums of one row of the gate begin where it does)
                 if (live) add(K::DG, c, fresh || (L < p.N && i % L == 0), o);
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) g[c][e] *= GATE ? p.scale * v.gate[c][e] : p.scale;
+            for (int e = 0; e < 8; ++e) g[c][e] *= GATE ? p.scale * v.gate[e] : p.scale;
             if constexpr (POST) {
                 if constexpr (FULL) {
 #pragma unroll
@@ -328,24 +360,32 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(BlockNormGrad p, C
                 }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    o[e] = g[c][e] * rh[c][e];
-                    g[c][e] *= wp[c][e];
-                    more[0] += g[c][e] * rh[c][e];
+                    o[e] = g[c][e] * rh[e];
+                    g[c][e] *= q.wp[e];
+                    more[0] += g[c][e] * rh[e];
                     if constexpr (FULL) more[1] += g[c][e];
                 }
                 if (live) add(K::DWP, c, fresh, o);
             }
         }
         // nothing of the row itself is needed from here on: the next row's values come while this one's second sums are formed
-        const float rho1 = v.rho1;
-        if (it + 1 < s.each) v = load(i + s.step);
+        const float m1 = u.m1, rho1 = u.rho1;
+        if (it + 1 < s.each) {
+            u = load_statistics(i + s.step);
+            if constexpr (C == 1) {
+                load_first(v, i + s.step, 0);
+                load_second(v, i + s.step, 0);
+            }
+        }
         if constexpr (POST) {
             row_sums<M, SMALL>(more, sh, turn, group * waves, waves);
             const float mky = more[0] * inv_h, mk = FULL && p.center ? more[1] * inv_h : 0.f;
 #pragma unroll
-            for (int c = 0; c < C; ++c)
+            for (int c = 0; c < C; ++c) {
+                if constexpr (C > 1) normed_y(load8((const T*)p.y + at, j[c]), m1, rho1);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) g[c][e] = rho1 * ((FULL ? g[c][e] - mk : g[c][e]) - rh[c][e] * mky);
+                for (int e = 0; e < 8; ++e) g[c][e] = rho1 * ((FULL ? g[c][e] - mk : g[c][e]) - rh[e] * mky);
+            }
         }
 #pragma unroll
         for (int c = 0; c < C; ++c)
@@ -356,18 +396,18 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(BlockNormGrad p, C
                                            : (i + 1) % L == 0 ? p.dgate + (size_t)k * p.h : s.tail + (size_t)c0 * s.pitch;
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                float q[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                if (C == 1 && K::DG < 2) {
+                float o8[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                if (K::in_registers(K::DG)) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        q[e] = reg[K::DG < 2 ? K::DG : 0][e];
-                        reg[K::DG < 2 ? K::DG : 0][e] = 0.f;
+                        o8[e] = in_reg(K::DG, c)[e];
+                        in_reg(K::DG, c)[e] = 0.f;
                     }
                 } else {
-                    kept(K::DG, c, false, q);
+                    kept(K::DG, c, false, o8);
                     if (K::DG < K::LDS1) slot(K::DG, c, 0) = slot(K::DG, c, 1) = make_float4(0.f, 0.f, 0.f, 0.f);
                 }
-                store8(o, j[c], skip[c], q);
+                store8(o, j[c], skip[c], o8);
             }
         }
     }
@@ -380,7 +420,13 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(BlockNormGrad p, C
             lds[1024 + threadIdx.x] = make_float4(reg[k][4], reg[k][5], reg[k][6], reg[k][7]);
         }
         float* out = matrix(k);
-        if (!out || (GATE && k == K::DG && L < p.N) || k >= (C == 1 ? K::COUNT : K::LDS1)) continue;
+        if (!out || (GATE && k == K::DG && L < p.N)) continue;
+        if (C > 1 && k >= K::LDS1) {      // (a workgroup is one group)
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                if (K::in_registers(k)) store8(out + (size_t)blockIdx.x * s.pitch, j[c], skip[c], in_reg(k, c));
+            continue;
+        }
         __syncthreads();
         const float* from = reinterpret_cast<const float*>(lds + (C == 1 && k < 2 ? 0 : (k - K::LDS0) * C * 2 * 1024));
         for (int col = threadIdx.x; col < p.h; col += blockDim.x) {

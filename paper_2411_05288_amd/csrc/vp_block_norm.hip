@@ -56,10 +56,10 @@ __device__ __forceinline__ Normed statistics(F f, int h, int center, float eps, 
 template <typename T>
 __global__ __launch_bounds__(1024) void block_norm_fwd_long_kernel(BlockNorm p) {
     __shared__ float sh[16];
-    for (int i = blockIdx.x; i < p.N; i += gridDim.x) {
+    for (int64_t i = blockIdx.x; i < p.N; i += gridDim.x) {
         const size_t row = (size_t)i * p.h;
         const T *x = (const T*)p.x + row, *y = p.y ? (const T*)p.y + row : nullptr;
-        const T* gate = p.gate ? (const T*)p.gate + (size_t)((int64_t)i * p.gate_rows / p.N) * p.h : nullptr;
+        const T* gate = p.gate ? (const T*)p.gate + (size_t)(i * p.gate_rows / p.N) * p.h : nullptr;
         Normed a{0.f, 1.f};
         if (p.post) a = statistics([&](int j) { return ld(y + j); }, p.h, p.center, p.eps, sh);
         auto sum = [&](int j) {
@@ -192,11 +192,11 @@ struct Row {
     const TD* dH;
     const TG* dr;
     float m1, rho1, m2, rho2;
-    __device__ Row(const BlockNormGrad& p, int i) {
+    __device__ Row(const BlockNormGrad& p, int64_t i) {
         const size_t row = (size_t)i * p.h;
         r = (const T*)p.r + row;
         y = p.y ? (const T*)p.y + row : nullptr;
-        gate = p.gate ? (const T*)p.gate + (size_t)((int64_t)i * p.gate_rows / p.N) * p.h : nullptr;
+        gate = p.gate ? (const T*)p.gate + (size_t)(i * p.gate_rows / p.N) * p.h : nullptr;
         dH = (const TD*)p.dH + row;
         dr = p.dr ? (const TG*)p.dr + row : nullptr;
         m1 = p.stats[i];
@@ -218,7 +218,7 @@ struct Row {
 template <typename T, typename TD, typename TG>
 __global__ __launch_bounds__(1024) void block_norm_bwd_means_kernel(BlockNormGrad p, float4* means) {
     __shared__ float sh[32];
-    for (int i = blockIdx.x; i < p.N; i += gridDim.x) {
+    for (int64_t i = blockIdx.x; i < p.N; i += gridDim.x) {
         const Row<T, TD, TG> q(p, i);
         float s[2] = {0.f, 0.f}, c[2] = {0.f, 0.f};
         for (int j = threadIdx.x; j < p.h; j += 1024) {
@@ -245,11 +245,11 @@ template <typename T, typename TD, typename TG>
 __global__ __launch_bounds__(256) void block_norm_bwd_columns_kernel(BlockNormGrad p, const float4* means, ColumnSums s) {
     const int j = blockIdx.x * 256 + threadIdx.x, c = blockIdx.y;
     if (j >= p.h) return;
-    const int i0 = c * s.each, i1 = i0 + s.each < p.N ? i0 + s.each : p.N;
+    const int64_t i0 = (int64_t)c * s.each, i1 = i0 + s.each < p.N ? i0 + s.each : p.N;
     const int L = p.gate_rows ? (int)(p.N / p.gate_rows) : 0;
     const float wp = ld_or((const T*)p.w_post, j, 1.f), bp = ld_or((const T*)p.b_post, j, 0.f);
     float dw = 0.f, db = 0.f, dwp = 0.f, dbp = 0.f, dg = 0.f;
-    for (int i = i0; i < i1; ++i) {
+    for (int64_t i = i0; i < i1; ++i) {
         const Row<T, TD, TG> q(p, i);
         const float4 m = means[i];
         const float dH = ld(q.dH + j), g = q.g(p, j, m.x, m.y);
@@ -262,10 +262,10 @@ __global__ __launch_bounds__(256) void block_norm_bwd_columns_kernel(BlockNormGr
         }
         if (p.dgate) {
             dg += p.scale * (p.post ? q.yh(j) * wp + bp : ld(q.y + j)) * g;
-            const int k = i / L;
+            const int64_t k = i / L;
             if (L == p.N) continue;
             if ((i + 1) % L == 0 || i + 1 == i1) {
-                if ((int64_t)k * L < i0) s.head[(size_t)c * s.pitch + j] = dg;
+                if (k * L < i0) s.head[(size_t)c * s.pitch + j] = dg;
                 else if ((i + 1) % L == 0) p.dgate[(size_t)k * p.h + j] = dg;
                 else s.tail[(size_t)c * s.pitch + j] = dg;
                 dg = 0.f;
@@ -283,7 +283,7 @@ __global__ __launch_bounds__(256) void block_norm_bwd_columns_kernel(BlockNormGr
 // Third step: dx and dy.
 template <typename T, typename TD, typename TG>
 __global__ __launch_bounds__(1024) void block_norm_bwd_rows_kernel(BlockNormGrad p, const float4* means) {
-    for (int i = blockIdx.x; i < p.N; i += gridDim.x) {
+    for (int64_t i = blockIdx.x; i < p.N; i += gridDim.x) {
         const Row<T, TD, TG> q(p, i);
         const float4 m = means[i];
         TG *dx = (TG*)p.dx + (size_t)i * p.h, *dy = p.dy ? (TG*)p.dy + (size_t)i * p.h : nullptr;
@@ -395,7 +395,7 @@ hipError_t launch_block_norm_fwd(const BlockNorm& p, vp_dtype dt, hipStream_t st
         else hipLaunchKernelGGL((block_norm_fwd_kernel<float, TR, C, false>), grid, block, 0, st, p);                          \
         return hipGetLastError();                                                                                              \
     } while (0)
-    if (p.h >= MIN_COLUMNS) {
+    if (p.h >= MIN_COLUMNS && p.N <= 1 << 27) {      // (a launch has less than 2^32 threads)
         if (p.h <= 128) VP_FWD(16, 1, 256);
         if (p.h <= 512) VP_FWD(64, 1, 256);
         if (p.h <= 1024) VP_FWD(64, 2, 256);

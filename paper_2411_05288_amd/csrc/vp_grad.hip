@@ -323,22 +323,20 @@ hipError_t launch_grad_call(const GradCall& a) {
     GradList l;
     l.n = l.at = l.first = 0;
     int64_t chunks = 0;
-    {
-        ProfScope prof(a.known ? K_GRAD_SCALE : K_GRAD_NORM, a.st);
-        for (int32_t k = 0; k < a.n; ++k) {
-            const GradTensor t{a.grads[k], a.outs ? a.outs[k] : const_cast<void*>(a.grads[k]),
-                               (uint64_t)a.counts[k] * 2 + (a.dts[k] == VP_BF16 ? 1 : 0)};
-            l.t[l.n++] = t;
-            chunks += t.chunks();
-            if (TABLE && (l.n == GRAD_LIST || k == a.n - 1)) {
-                hipLaunchKernelGGL(grad_table_kernel, dim3(1), dim3(64), 0, a.st, l, a.table);
-                l.at = k + 1;
-                l.first = (int)chunks;
-                l.n = 0;
-            }
+    for (int32_t k = 0; k < a.n; ++k) {
+        const GradTensor t{a.grads[k], a.outs ? a.outs[k] : const_cast<void*>(a.grads[k]),
+                           (uint64_t)a.counts[k] * 2 + (a.dts[k] == VP_BF16 ? 1 : 0)};
+        l.t[l.n++] = t;
+        chunks += t.chunks();
+        if (TABLE && (l.n == GRAD_LIST || k == a.n - 1)) {
+            ProfScope prof(a.known ? K_GRAD_SCALE : K_GRAD_NORM, a.st);
+            hipLaunchKernelGGL(grad_table_kernel, dim3(1), dim3(64), 0, a.st, l, a.table);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+            l.at = k + 1;
+            l.first = (int)chunks;
+            l.n = 0;
         }
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
     }
     const int blocks = chunks < 1 ? 1 : chunks < GRAD_BLOCKS ? (int)chunks : GRAD_BLOCKS;
     if (!a.known) {

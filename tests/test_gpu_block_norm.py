@@ -312,3 +312,75 @@ def test_bf16_as_bit_patterns():
     vp.vp_block_norm_fwd(s["x"], None, a, w=s["w"])
     vp.vp_block_norm_fwd(s["x"].view(torch.int16), None, b, w=s["w"])
     assert torch.equal(a, b)
+
+
+def test_offsets_beyond_32_bits():
+    """The rows at both ends of tensors of more than 2^32 bytes."""
+    import paper_2411_05288_amd as vp
+    N, h = 262149, 4100
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, y = (torch.randn(N, h, generator=g, device="cuda") for _ in range(2))
+    assert x.numel() * 4 > 1 << 32
+    H, r, stats = torch.empty_like(x), torch.empty_like(x), torch.empty(4, N, device="cuda")
+    vp.vp_block_norm_fwd(x, y, H, r=r, stats=stats, post=True, center=True)
+    ends = torch.tensor([0, 1, N // 2, N - 2, N - 1], device="cuda")
+    for name, (value, bound) in ref.forward(x[ends], y[ends], post=True, center=True).items():
+        ref.check(name, {"r": r[ends], "H": H[ends], "stats": stats[:, ends]}[name], value, bound)
+    dr = x      # (any values)
+    dx, dy = torch.empty_like(x), torch.empty_like(x)
+    ws = torch.empty(vp.vp_block_norm_bwd_workspace_bytes(N, h, post=True), dtype=torch.uint8, device="cuda")
+    vp.vp_block_norm_bwd(H, r, y, stats, dr=dr, dx=dx, dy=dy, post=True, center=True, workspace=ws)
+    expected = ref.backward(H[ends], r[ends], y[ends], stats[:, ends], dr=dr[ends], post=True, center=True)
+    ref.check("dx", dx[ends], *expected["dx"])
+    ref.check("dy", dy[ends], *expected["dy"])
+
+
+@pytest.mark.parametrize("N,h", [(1500, 264), (40, 9000), (300, 5)])
+def test_two_streams_at_once(N, h):
+    """Calls that overlap, each with buffers and a workspace of its own."""
+    import paper_2411_05288_amd as vp
+    s = inputs(N, h, BF16, True, 1, True, 9)
+    plans = [vp.BlockNormPlan(s["x"], s["y"], gate=s["gate"], w=s["w"], b=s["b"], w_post=s["w_post"], b_post=s["b_post"], post=True) for _ in range(3)]
+    dH = torch.randn(N, h, device="cuda")
+    streams = [torch.cuda.Stream() for _ in plans]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for plan, stream in zip(plans, streams):
+            plan.forward(stream)
+            plan.backward(dH, stream=stream)
+    torch.cuda.synchronize()
+    for plan in plans[1:]:
+        for a, b in zip([plan.r, plan.H, plan.stats, plan.dx, plan.dy] + plan.parameter_gradients(),
+                        [plans[0].r, plans[0].H, plans[0].stats, plans[0].dx, plans[0].dy] + plans[0].parameter_gradients()):
+            assert torch.equal(a, b)
+
+
+TYPES = [(F32, F32, F32), (BF16, F32, F32), (BF16, F32, BF16), (BF16, BF16, F32), (BF16, BF16, BF16)]
+
+
+@pytest.mark.parametrize("dtype,dH_type,grad", TYPES)
+@pytest.mark.parametrize("post,bias", list(itertools.product((False, True), repeat=2)))
+@pytest.mark.parametrize("N,h,gate", [(N, h, gate) for N, h in ((612, 90), (36, 1043), (612, 520), (36, 8203), (36, 4))
+                                      for gate in (0, 1, 4, 36, 612) if not gate or N % gate == 0])
+def test_every_backward_kernel(N, h, post, gate, bias, dtype, dH_type, grad):
+    """All types and parts at rows of lanes, wavefronts and a workgroup, two vectors per thread, and lengths below a vector; a
+    gate per channel, per token, and with rows that lie within and across what a group of threads sums."""
+    import paper_2411_05288_amd as vp
+    seed = h + 2 * gate + bias
+    s = inputs(N, h, dtype, post, gate, bias, seed)
+    opts = dict(gate=s["gate"], w_post=s["w_post"], b_post=s["b_post"], scale=0.75, post=post, center=bias)
+    H, r, stats = torch.empty_like(s["x"]), torch.empty_like(s["x"]), torch.empty(4, N, device="cuda")
+    vp.vp_block_norm_fwd(s["x"], s["y"], H, r=r, stats=stats, w=s["w"], b=s["b"], **opts)
+    dH, dr = torch.randn(N, h, device="cuda").to(dH_type), torch.randn(N, h, device="cuda").to(grad)
+    shapes = {"dx": ((N, h), grad), "dy": ((N, h), grad), "dgate": ((gate, h), F32)}
+    want = ["dx", "dy", "dw"] + (["db"] if bias else []) + (["dgate"] if gate else [])
+    want += (["dw_post"] + (["db_post"] if bias else [])) if post else []
+    out = {k: guarded(*shapes.get(k, ((h,), F32))) for k in want}
+    size = vp.vp_block_norm_bwd_workspace_bytes(N, h, gate, post)
+    ws, ws_ok = guarded((size,), torch.uint8, 0xFF)
+    vp.vp_block_norm_bwd(dH, r, s["y"], stats, dr=dr, w=s["w"], workspace=ws, **{k: t for k, (t, _) in out.items()}, **opts)
+    expected = ref.backward(dH, r, s["y"], stats, dr=dr, w=s["w"], grad_dtype=grad, **opts)
+    for name in want:
+        ref.check(name, out[name][0], *expected[name])
+        assert out[name][1](), name
+    assert ws_ok()

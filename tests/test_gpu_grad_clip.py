@@ -227,3 +227,18 @@ def test_training_step_from_norm_to_clipping():
     embed.dtable[0].mul_(3.0)
     plan.clip_gradients(total / 3, embed.dtable)
     assert plan.clip_plan is first
+
+
+def test_a_tensor_of_more_than_32_bits_of_bytes():
+    import paper_2411_05288_amd as vp
+    n = (1 << 30) + 5000
+    big, small = torch.full((n,), 0.5, device="cuda"), torch.full((3,), 2.0, device="cuda")
+    big[-1], big[1 << 30] = 3.0, -4.0
+    norm, ws = torch.empty(1, device="cuda"), torch.empty(vp.vp_grad_workspace_bytes(2), dtype=torch.uint8, device="cuda")
+    vp.vp_grad_clip([big, small], 1.0, norm, ws)
+    expected = math.sqrt((n - 2) * 0.25 + 9 + 16 + 12)
+    assert abs(float(norm) - expected) <= 2.0 ** -23 * expected
+    f = 1 / expected
+    for at, value in ((0, 0.5), (12345678, 0.5), (1 << 30, -4.0), (n - 2, 0.5), (n - 1, 3.0)):
+        assert abs(float(big[at]) - value * f) <= 4 * 2.0 ** -24 * abs(value * f)
+    assert int((big != big[0]).sum()) == 2 and abs(float(small[2]) - 2 * f) <= 8 * 2.0 ** -24 * f
