@@ -18,7 +18,7 @@ namespace vp {
 namespace {
 constexpr int GRAD_LIST = 160;              // tensors in the kernel arguments
 constexpr int GRAD_CHUNK_BYTES = 32768;     // 256 threads, eight loads of 16 bytes each
-constexpr int GRAD_BLOCKS = 1024;           // partial sums at most
+constexpr int GRAD_BLOCKS = 1024;           // workgroups, and partial sums, at most
 constexpr int GRAD_KEEP = (192 << 20) / GRAD_CHUNK_BYTES;      // chunks that the infinity cache holds from one launch to the next
 constexpr int GRAD_FIRSTS = 2048;           // numbers of first chunks that a workgroup holds in LDS
 
@@ -41,9 +41,22 @@ struct GradTable {      // more tensors than the arguments hold: entries and the
     int* first;
 };
 
-// Element-aligned vectors of 16 bytes: gradients may be views that start anywhere.
-typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
-typedef unsigned short u16x8u __attribute__((ext_vector_type(8), aligned(2)));
+// Vectors of 16 bytes at the alignment of an element: gradients may be views that start anywhere.  In registers they are words
+// (vectors of 16-bit elements that are loaded under a condition take a register per element, words at odd addresses a load per
+// element).
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <typename T>
+struct Vec;
+template <>
+struct Vec<float> {
+    typedef float type __attribute__((ext_vector_type(4), aligned(4)));
+    typedef float loaded __attribute__((ext_vector_type(4)));
+};
+template <>
+struct Vec<u16> {
+    typedef unsigned short type __attribute__((ext_vector_type(8), aligned(2)));
+    typedef unsigned short loaded __attribute__((ext_vector_type(8)));
+};
 
 // (an address from the table is one of global memory)
 template <typename T>
@@ -141,88 +154,135 @@ struct Tensors {
     }
 };
 
-__device__ __forceinline__ float bf16_to_f32(unsigned short b) { return __uint_as_float((unsigned)b << 16); }
-__device__ __forceinline__ unsigned short f32_to_bf16(float v) {
+__device__ __forceinline__ float bits(uint32_t b) { return __uint_as_float(b); }
+__device__ __forceinline__ uint32_t bf16_bits(float v) {
     const __bf16 b = (__bf16)v;
     return __builtin_bit_cast(unsigned short, b);
 }
 
-__device__ __forceinline__ void add_squares(double* s, f32x4u v) {
+// s += squares of the elements of a vector, in fp64
+template <typename T>
+__device__ __forceinline__ void add_squares(double* s, u32x4 v) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) s[e & 1] = fma((double)v[e], (double)v[e], s[e & 1]);
-}
-__device__ __forceinline__ void add_squares(double* s, u16x8u v) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const double d = bf16_to_f32(v[e]);
-        s[e & 1] = fma(d, d, s[e & 1]);
-    }
-}
-
-// Squares of a tensor's chunk.
-template <bool KEEP, typename V, typename T>
-__device__ __forceinline__ void chunk_squares(const T* g, int64_t count, int within, double* s) {
-    constexpr int E = 16 / sizeof(T), CHUNK = GRAD_CHUNK_BYTES / sizeof(T), STEPS = CHUNK / (256 * E);
-    const int64_t e0 = (int64_t)within * CHUNK, left = count - e0;
-    const T* p = global(g) + e0 + threadIdx.x * E;
-    if (left >= CHUNK) {
-        V v[STEPS];
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
-            const V* at = reinterpret_cast<const V*>(p + i * 256 * E);
-            v[i] = KEEP ? *at : __builtin_nontemporal_load(at);
-        }
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) add_squares(s, v[i]);
-        return;
-    }
-    const int n = (int)left;
-    for (int j = threadIdx.x * E; j < n; j += 256 * E, p += 256 * E) {
-        if (j + E <= n) {
-            add_squares(s, *reinterpret_cast<const V*>(p));
+    for (int e = 0; e < 4; ++e) {
+        if constexpr (sizeof(T) == 4) {
+            const double d = bits(v[e]);
+            s[e & 1] = fma(d, d, s[e & 1]);
         } else {
-            V v = {};
-            for (int e = 0; j + e < n; ++e) v[e] = p[e];
-            add_squares(s, v);
+            const double low = bits(v[e] << 16), high = bits(v[e] & 0xffff0000u);
+            s[0] = fma(low, low, s[0]);
+            s[1] = fma(high, high, s[1]);
         }
     }
 }
-
-__device__ __forceinline__ f32x4u times(f32x4u v, float f) { return v * f; }
-__device__ __forceinline__ u16x8u times(u16x8u v, float f) {
-    u16x8u o;
+// the elements times f, rounded to the type
+template <typename T>
+__device__ __forceinline__ u32x4 times(u32x4 v, float f) {
+    u32x4 o;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = f32_to_bf16(bf16_to_f32(v[e]) * f);
+    for (int e = 0; e < 4; ++e) {
+        if constexpr (sizeof(T) == 4) o[e] = __float_as_uint(bits(v[e]) * f);
+        else o[e] = bf16_bits(bits(v[e] << 16) * f) | bf16_bits(bits(v[e] & 0xffff0000u) * f) << 16;
+    }
     return o;
 }
-__device__ __forceinline__ float times1(float v, float f) { return v * f; }
-__device__ __forceinline__ unsigned short times1(unsigned short v, float f) { return f32_to_bf16(bf16_to_f32(v) * f); }
+__device__ __forceinline__ uint32_t word_of(float v) { return __float_as_uint(v); }
+__device__ __forceinline__ uint32_t word_of(u16 v) { return v; }
 
-template <bool STREAM, typename V, typename T>
-__device__ __forceinline__ void chunk_scale(const T* g, T* o, int64_t count, int within, float f) {
-    constexpr int E = 16 / sizeof(T), CHUNK = GRAD_CHUNK_BYTES / sizeof(T), STEPS = CHUNK / (256 * E);
-    const int64_t e0 = (int64_t)within * CHUNK, left = count - e0;
-    const T* p = global(g) + e0 + threadIdx.x * E;
-    T* q = global(o) + e0 + threadIdx.x * E;
-    if (left >= CHUNK) {
-        V v[STEPS];
+// A tensor's chunk.  At the end of a tensor the vectors that are whole are asked for four at a time, the elements behind them go to a thread each.
+template <typename T>
+struct Chunk {
+    static constexpr int E = 16 / sizeof(T), SIZE = GRAD_CHUNK_BYTES / sizeof(T), STEPS = SIZE / (256 * E);
+    int64_t first;      // element
+    int n;              // elements
+    __device__ Chunk(int64_t count, int within) {
+        first = (int64_t)within * SIZE;
+        n = count - first < SIZE ? (int)(count - first) : SIZE;
+    }
+    __device__ bool whole() const { return n == SIZE; }
+    __device__ static int at(int step) { return (step * 256 + threadIdx.x) * E; }
+    __device__ bool has(int step) const { return at(step) + E <= n; }
+    // the element behind the whole vectors that is this thread's, or -1
+    __device__ int rest() const { return (int)threadIdx.x < n % E ? n / E * E + threadIdx.x : -1; }
+};
+
+template <bool KEEP, typename T>
+__device__ __forceinline__ void chunk_squares(const T* g, int64_t count, int within, double* s) {
+    using C = Chunk<T>;
+    using V = typename Vec<T>::type;
+    const C c(count, within);
+    const T* p = global(g) + c.first;
+    auto load = [&](int i) -> u32x4 {
+        const V* at = reinterpret_cast<const V*>(p + C::at(i));
+        const typename Vec<T>::loaded v = KEEP ? *at : __builtin_nontemporal_load(at);
+        return __builtin_bit_cast(u32x4, v);
+    };
+    if (c.whole()) {
+        u32x4 v[C::STEPS];
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) v[i] = __builtin_nontemporal_load(reinterpret_cast<const V*>(p + i * 256 * E));
+        for (int i = 0; i < C::STEPS; ++i) v[i] = load(i);
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
-            V* at = reinterpret_cast<V*>(q + i * 256 * E);
-            if constexpr (STREAM) __builtin_nontemporal_store(times(v[i], f), at);
-            else *at = times(v[i], f);
-        }
+        for (int i = 0; i < C::STEPS; ++i) add_squares<T>(s, v[i]);
         return;
     }
-    const int n = (int)left;
-    for (int j = threadIdx.x * E; j < n; j += 256 * E, p += 256 * E, q += 256 * E) {
-        if (j + E <= n) {
-            *reinterpret_cast<V*>(q) = times(*reinterpret_cast<const V*>(p), f);
-        } else {
-            for (int e = 0; j + e < n; ++e) q[e] = times1(p[e], f);
+    u32x4 rest = {};
+    if (c.rest() >= 0) rest[0] = word_of(p[c.rest()]);
+    for (int k = 0; k < C::STEPS && C::at(k) - C::at(0) < c.n; k += 4) {
+        u32x4 v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] = u32x4{};
+            if (c.has(k + i)) v[i] = load(k + i);
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) add_squares<T>(s, v[i]);
+    }
+    add_squares<T>(s, rest);
+}
+
+template <bool STREAM, typename T>
+__device__ __forceinline__ void chunk_scale(const T* g, T* o, int64_t count, int within, float f) {
+    using C = Chunk<T>;
+    using V = typename Vec<T>::type;
+    const C c(count, within);
+    const T* p = global(g) + c.first;
+    T* q = global(o) + c.first;
+    auto load = [&](int i) {
+        const typename Vec<T>::loaded v = __builtin_nontemporal_load(reinterpret_cast<const V*>(p + C::at(i)));
+        return __builtin_bit_cast(u32x4, v);
+    };
+    auto store = [&](int i, u32x4 v) {
+        V* at = reinterpret_cast<V*>(q + C::at(i));
+        const auto w = __builtin_bit_cast(typename Vec<T>::loaded, v);
+        if constexpr (STREAM) __builtin_nontemporal_store((V)w, at);
+        else *at = w;
+    };
+    if (c.whole()) {
+        u32x4 v[C::STEPS];
+#pragma unroll
+        for (int i = 0; i < C::STEPS; ++i) v[i] = load(i);
+#pragma unroll
+        for (int i = 0; i < C::STEPS; ++i) store(i, times<T>(v[i], f));
+        return;
+    }
+    const int rest = c.rest();
+    u32x4 last = {};
+    if (rest >= 0) last[0] = word_of(p[rest]);
+    for (int k = 0; k < C::STEPS && C::at(k) - C::at(0) < c.n; k += 4) {
+        u32x4 v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] = u32x4{};
+            if (c.has(k + i)) v[i] = load(k + i);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c.has(k + i)) store(k + i, times<T>(v[i], f));
+    }
+    if (rest >= 0) {
+        const uint32_t w = times<T>(last, f)[0];
+        if constexpr (sizeof(T) == 4) q[rest] = bits(w);
+        else q[rest] = (u16)w;
     }
 }
 
@@ -257,11 +317,11 @@ __global__ __launch_bounds__(256) void grad_squares_kernel(GradList l, GradTable
         int within;
         const GradTensor t = ts.of(c, within);
         if (c >= keep) {
-            if (t.bf16()) chunk_squares<true, u16x8u>((const u16*)t.g, t.count(), within, s);
-            else chunk_squares<true, f32x4u>((const float*)t.g, t.count(), within, s);
+            if (t.bf16()) chunk_squares<true>((const u16*)t.g, t.count(), within, s);
+            else chunk_squares<true>((const float*)t.g, t.count(), within, s);
         } else {
-            if (t.bf16()) chunk_squares<false, u16x8u>((const u16*)t.g, t.count(), within, s);
-            else chunk_squares<false, f32x4u>((const float*)t.g, t.count(), within, s);
+            if (t.bf16()) chunk_squares<false>((const u16*)t.g, t.count(), within, s);
+            else chunk_squares<false>((const float*)t.g, t.count(), within, s);
         }
     }
     const double sum = block_sum64(s[0] + s[1], sh);
@@ -286,6 +346,7 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(GradList l, GradTable t
                                                          const double* part, int parts, float max_norm, float* norm) {
     __shared__ double sh[4];
     __shared__ int firsts[TABLE ? GRAD_FIRSTS : 1];
+    const Tensors<TABLE> ts(l, table, n, firsts);      // (their first chunks arrive while the norm does)
     float v;
     if (parts) {
         v = norm_of(part, parts, sh);
@@ -295,12 +356,11 @@ __global__ __launch_bounds__(256) void grad_scale_kernel(GradList l, GradTable t
     }
     const float f = v > max_norm && v < INFINITY ? max_norm / v : 1.f;
     if (f == 1.f && in_place) return;
-    const Tensors<TABLE> ts(l, table, n, firsts);
     for (int c = chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
         int within;
         const GradTensor t = ts.of(c, within);
-        if (t.bf16()) chunk_scale<STREAM, u16x8u>((const u16*)t.g, (u16*)t.o, t.count(), within, f);
-        else chunk_scale<STREAM, f32x4u>((const float*)t.g, (float*)t.o, t.count(), within, f);
+        if (t.bf16()) chunk_scale<STREAM>((const u16*)t.g, (u16*)t.o, t.count(), within, f);
+        else chunk_scale<STREAM>((const float*)t.g, (float*)t.o, t.count(), within, f);
     }
 }
 
