@@ -124,7 +124,7 @@ __device__ __forceinline__ void row_sums(float* v, float (*sh)[K_ROW_SUMS], int&
 #pragma unroll
             for (int k = 0; k < K; ++k) at[(threadIdx.x >> 6) * K + k] = v[k];
         __syncthreads();
-const int l = threadIdx.x & 15;      // (at most 16 wavefronts)
+        const int l = threadIdx.x & 15;      // (at most 16 wavefronts)
 #pragma unroll
         for (int k = 0; k < K; ++k) v[k] = sum16(l < waves ? at[(wave0 + l) * K + k] : 0.f);
     }
@@ -132,8 +132,9 @@ const int l = threadIdx.x & 15;      // (at most 16 wavefronts)
 
 // The sums over tokens: `ranges` groups of threads (`rows` groups of `threads` threads in a workgroup) take up to `each` rows, one
 // at a time: group c rows c, c + ranges, ... (`step` = ranges: what the chip reads at one time lies together), or, under a gate of
-// several rows, `each` rows from c * each on (step = 1), so that a row of the gate has few groups to be summed over.  What workgroup b has summed goes to row b of the partial matrices (there are
-// `parts`), which a last launch adds up in order; with a single workgroup it goes to the results themselves.
+// several rows, `each` rows from c * each on (step = 1), so that a row of the gate has few groups to be summed over.  What
+// workgroup b has summed goes to row b of the partial matrices (there are `parts`), which a last launch adds up in order; with a
+// single workgroup it goes to the results themselves.
 // dgate with several rows: a row of the gate whose tokens lie in one range is written where it ends; one that continues in the
 // next range goes to row c of `tail`, one that began before (and ends or continues) to row c of `head`, c the range.
 struct ColumnSums {

@@ -16,6 +16,7 @@
 namespace vp {
 
 namespace {
+
 constexpr int GRAD_LIST = 160;              // tensors in the kernel arguments
 constexpr int GRAD_CHUNK_BYTES = 32768;     // 256 threads, eight loads of 16 bytes each
 constexpr int GRAD_BLOCKS = 1024;           // workgroups, and partial sums, at most

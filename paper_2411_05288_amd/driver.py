@@ -40,7 +40,8 @@ class BlockNormPlan:
     makes layer norms of RMS norms; y=None: H = norm(x) alone), and the gradients of all of it.
 
     ``train=False`` keeps no statistics and no buffers for gradients: ``forward`` alone, as for single tokens.  Gradients of
-    activations (dx, dy) are of ``grad_dtype`` (default: the type of x), those of parameters fp32."""
+    activations (dx, dy) are of ``grad_dtype`` (default: the type of x), those of parameters fp32.  A plan's calls share its
+    buffers: they belong on one stream, or one after the other."""
 
     def __init__(self, x: torch.Tensor, y: Optional[torch.Tensor] = None, *, gate=None, w=None, b=None, w_post=None, b_post=None,
                  scale: float = 1.0, eps: float = 1e-5, post: bool = False, center: bool = False, grad_dtype=None,
@@ -83,7 +84,8 @@ class BlockNormPlan:
 class GradientClipPlan:
     """The norm of many gradients together, and clipping by it: the gradients of all layers of a step, of fp32 or bf16, in place
     or into ``outs`` (tensors of their types and shapes, views of one flat buffer among them).  The plan keeps the tensors'
-    addresses: a gradient that moves needs a new plan."""
+    addresses: a gradient that moves needs a new plan.  A plan's calls share its workspace and ``norm``: they belong on one
+    stream, or one after the other."""
 
     def __init__(self, grads: List[torch.Tensor], outs: Optional[List[torch.Tensor]] = None):
         self.arguments = B.GradientArguments(grads, outs)
