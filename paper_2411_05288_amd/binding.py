@@ -9,7 +9,6 @@ twice as long).  The library has no fallback: if it is missing or a call fails, 
 """
 from __future__ import annotations
 
-import bisect
 import ctypes
 import importlib.util
 import os
@@ -632,29 +631,28 @@ class GradientArguments:
         n = self.n = len(self.grads)
         if outs is not None and len(self.outs) != n:
             raise VPError("outs: one tensor per gradient")
-        self.ptrs = (ctypes.c_void_p * n)(*[_ptr(g, "grads") for g in self.grads])
-        self.counts = (ctypes.c_int64 * n)(*[g.numel() for g in self.grads])
-        self.dts = (ctypes.c_int32 * n)(*[_dtype_code(g) for g in self.grads])
-        self.out_ptrs = None
-        if outs is not None:
-            self.out_ptrs = (ctypes.c_void_p * n)(*[_ptr(o, "outs", (g.dtype,), g.shape) for g, o in zip(self.grads, self.outs)])
+        ptrs = [_ptr(g, "grads") for g in self.grads]
+        counts = [g.numel() for g in self.grads]
+        dts = [_dtype_code(g) for g in self.grads]
+        out_ptrs = None if outs is None else [_ptr(o, "outs", (g.dtype,), g.shape) for g, o in zip(self.grads, self.outs)]
         if len({t.get_device() for t in self.grads + (self.outs or [])}) > 1:
             raise VPError("gradients of one call are on one device")
         self.first = self.grads[0] if n else None
-        # What is written is written by no order: outputs are apart from one another and from all gradients but their own.
-        written = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), k)
-                         for k, t in enumerate(self.grads if outs is None else self.outs) if t.numel())
-        self.overlap = any(a[1] > b[0] for a, b in zip(written, written[1:]))
-        if outs is not None and not self.overlap:
-            starts = [a[0] for a in written]
-            for k, g in enumerate(self.grads):
-                first, end = g.data_ptr(), g.data_ptr() + g.numel() * g.element_size()
-                at = bisect.bisect_right(starts, first) - 1
-                for a in written[max(at, 0):]:
-                    if a[0] >= end:
-                        break
-                    if a[1] > first and first < end and not (a[2] == k and a[0] == first):
-                        self.overlap = True
+        self.ptrs, self.counts, self.dts = (ctypes.c_void_p * n)(*ptrs), (ctypes.c_int64 * n)(*counts), (ctypes.c_int32 * n)(*dts)
+        self.out_ptrs = None if outs is None else (ctypes.c_void_p * n)(*out_ptrs)
+        # What is written is written in no order: outputs are apart from one another and from all gradients but their own.
+        sizes = [c * (2 if d == VP_BF16 else 4) for c, d in zip(counts, dts)]
+        spans = [(p, z, True) for p, z in zip(ptrs if outs is None else out_ptrs, sizes) if z]
+        if outs is not None:
+            spans += [(p, z, False) for p, z, o in zip(ptrs, sizes, out_ptrs) if z and p != o]
+        read = written = 0      # ends of the spans before
+        self.overlap = False
+        for start, size, is_written in sorted(spans):
+            self.overlap |= start < written or (is_written and start < read)
+            if is_written:
+                written = max(written, start + size)
+            else:
+                read = max(read, start + size)
 
 
 def _grad_call(name: str, a, norm, workspace, stream, max_norm=None):

@@ -340,7 +340,7 @@ __global__ __launch_bounds__(256) void block_norm_bwd_sum_kernel(BlockNormGrad p
         }
     sh[slice][threadIdx.x & 7] = v;
     __syncthreads();
-    if (threadIdx.x < 32 && blockIdx.x * 32 + threadIdx.x < p.h) {
+    if (threadIdx.x < 32 && (int)(blockIdx.x * 32 + threadIdx.x) < p.h) {
         float sum = 0.f;
 #pragma unroll
         for (int q = 0; q < 32; ++q) sum += reinterpret_cast<const float*>(sh[q])[threadIdx.x];
@@ -369,8 +369,10 @@ ColumnSums cut(int64_t N, int64_t h, int64_t gate_rows) {
     s.each = (int)ceil_div(N, parts * s.rows);
     s.ranges = (int)ceil_div(N, s.each);
     s.parts = (int)ceil_div(s.ranges, s.rows);
-    if (bwd_in_one_pass(h)) {      // few rows: on as many CUs as there are
-        s.rows = (int)ceil_div(s.ranges, CUS);
+    if (bwd_in_one_pass(h)) {
+        // few rows: on one CU, if it holds all of them at once (nothing is left to add up then: N=16 h=256 7.1 -> 5.2 us), else on as
+        // many CUs as there are
+        s.rows = s.ranges <= s.rows ? s.ranges : (int)ceil_div(s.ranges, CUS);
         s.parts = (int)ceil_div(s.ranges, s.rows);
     }
     if (bwd_in_one_pass(h) && (gate_rows <= 1 || gate_rows == N)) s.step = s.ranges = s.parts * s.rows;

@@ -242,3 +242,43 @@ def test_a_tensor_of_more_than_32_bits_of_bytes():
     for at, value in ((0, 0.5), (12345678, 0.5), (1 << 30, -4.0), (n - 2, 0.5), (n - 1, 3.0)):
         assert abs(float(big[at]) - value * f) <= 4 * 2.0 ** -24 * abs(value * f)
     assert int((big != big[0]).sum()) == 2 and abs(float(small[2]) - 2 * f) <= 8 * 2.0 ** -24 * f
+
+
+@pytest.mark.parametrize("algorithm", [1, 2])
+def test_step_with_norm_and_clipping_in_a_graph(algorithm):
+    """bf16, layer norms with a gate per sequence: the whole step and the clipping, eager and replayed, bit for bit."""
+    import paper_2411_05288_amd as vp
+    N, h, V, p = 240, 512, 1536, 3
+    g = torch.Generator(device="cuda").manual_seed(4)
+
+    def normal(*shape, std=1.0, mean=0.0):
+        return (torch.randn(*shape, generator=g, device="cuda") * std + mean).bfloat16()
+    norm = vp.BlockNormPlan(normal(N, h), normal(N, h), gate=normal(4, h), w=normal(h, mean=1.0, std=0.1), b=normal(h), post=True,
+                            w_post=normal(h, mean=1.0, std=0.1), b_post=normal(h), center=True, scale=0.5)
+    labels = torch.randint(0, V, (N,), generator=g, device="cuda")
+    plan = vp.OutputLayerPlan(None, [normal(V // p, h, std=0.05) for _ in range(p)], labels, norm=norm, algorithm=algorithm)
+    other = normal(1001)
+    kept = other.clone()
+
+    def step():
+        other.copy_(kept)
+        plan.step()
+        return plan.clip_gradients(0.01, [other])
+    total = step()
+    torch.cuda.synchronize()
+    outs = [plan.loss, norm.H, norm.r, norm.dx, norm.dy, total, other, *norm.parameter_gradients(), *plan.dW]
+    expected = [t.clone() for t in outs]
+    assert float(total) > 0.01 and all(bool(torch.isfinite(t).all()) for t in outs)
+    clipped = exact_norm([other, *norm.parameter_gradients(), *plan.dW])
+    assert abs(clipped - 0.01) <= 0.01 * 2.0 ** -8      # (the bf16 one rounds its elements by half a step at most)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        for t in outs + [plan.workspace, norm.workspace, plan.clip_plan.workspace]:
+            t.fill_(float("nan") if t.is_floating_point() else 0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, expected))
+        assert float(torch.arange(1000, device="cuda", dtype=torch.float32).sum()) == 499500.0
