@@ -282,3 +282,59 @@ def test_step_with_norm_and_clipping_in_a_graph(algorithm):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, expected))
         assert float(torch.arange(1000, device="cuda", dtype=torch.float32).sum()) == 499500.0
+
+
+def test_plan_scales_by_a_norm_over_several_devices():
+    """What a program with its gradients on several devices does: norms joined outside, every device scales by the whole."""
+    import paper_2411_05288_amd as vp
+    parts = [[g for _, g in make([(5000, F32, 0), (333, BF16, 1)], seed=s)] for s in (1, 2)]
+    before = [[g.clone() for g in part] for part in parts]
+    plans = [vp.GradientClipPlan(part) for part in parts]
+    for plan in plans:
+        plan.compute_norm()
+    whole = torch.stack([plan.norm.double() ** 2 for plan in plans]).sum(0).sqrt().float()
+    expected = exact_norm([g for part in before for g in part])
+    assert abs(float(whole) - expected) <= 2.0 ** -22 * expected
+    for plan in plans:
+        plan.scale(2.0, whole)
+    for part, old in zip(parts, before):
+        for g, b in zip(part, old):      # the joined norm has two roundings more
+            value = b.double() * (2.0 / expected)
+            assert bool(((g.double() - value).abs() <= value.abs() * (8 * 2.0 ** -24 + (HALF[BF16] if g.dtype == BF16 else 0))).all())
+    plans[0].compute_norm()
+    mine = float(plans[0].norm)
+    plans[0].scale(mine / 4)
+    assert abs(exact_norm(parts[0]) - mine / 4) <= mine * 2.0 ** -8
+
+
+def test_plan_notices_gradients_that_moved():
+    import paper_2411_05288_amd as vp
+    W = [torch.randn(64, 32, device="cuda")]
+    plan = vp.OutputLayerPlan(torch.randn(16, 32, device="cuda"), W, torch.zeros(16, dtype=torch.int64, device="cuda"))
+    plan.step()
+    other = torch.randn(100, device="cuda")
+    plan.clip_gradients(1e-3, [other])
+    first = plan.clip_plan
+    plan.clip_gradients(1e-3, [other])
+    assert plan.clip_plan is first
+    other.data = torch.randn(100, device="cuda")      # the same tensor, other memory
+    total = plan.clip_gradients(1e-4, [other])
+    assert plan.clip_plan is not first and float(total) > 1
+    assert abs(exact_norm([other, *plan.dW]) - 1e-4) <= 1e-9
+
+
+def test_evaluation_with_a_norm_that_keeps_nothing():
+    import paper_2411_05288_amd as vp
+    N, h, V = 5, 256, 640
+    x, y = torch.randn(N, h, device="cuda").bfloat16(), torch.randn(N, h, device="cuda").bfloat16()
+    W = [torch.randn(V // 2, h, device="cuda").bfloat16() for _ in range(2)]
+    labels = torch.arange(N, device="cuda")
+    losses = []
+    for train in (True, False):
+        norm = vp.BlockNormPlan(x, y, post=True, train=train)
+        plan = vp.OutputLayerPlan(None, W, labels, save_logits=False, norm=norm)
+        plan.forward()
+        losses.append(plan.loss.clone())
+    assert torch.equal(*losses) and norm.stats is None
+    with pytest.raises(vp.VPError, match="train=False"):
+        plan.backward()
