@@ -105,19 +105,23 @@ __device__ __forceinline__ float sum16(float v) {
     return add_rotated<1>(add_rotated<2>(add_rotated<4>(add_rotated<8>(v))));
 }
 __device__ __forceinline__ float lane(float v, int l) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), l)); }
+__device__ __forceinline__ float sum32(float v) {      // (two halves of a wavefront, each in all of its lanes)
+    v = sum16(v);
+    return v + __shfl_xor(v, 16, 64);
+}
 __device__ __forceinline__ float sum64(float v) {
     v = sum16(v);
     return (lane(v, 0) + lane(v, 16)) + (lane(v, 32) + lane(v, 48));
 }
 
-// Sums of K values over the threads of a row, a fixed tree: SMALL rows are held by 16 lanes, others by `waves` whole wavefronts of
-// the workgroup, the first of them `wave0`.  Several meet in LDS, in the half of `sh` that `turn` names (so that one barrier per
+// Sums of K values over the threads of a row, a fixed tree: rows are held by 16 or 32 LANES, or (LANES = 64) by `waves` whole
+// wavefronts of the workgroup, the first of them `wave0`.  Several meet in LDS, in the half of `sh` that `turn` names (so that one barrier per
 // sum is enough: a thread that writes a half has passed the barrier behind which all others have read what it held).
-template <int K, bool SMALL>
+template <int K, int LANES>
 __device__ __forceinline__ void row_sums(float* v, float (*sh)[K_ROW_SUMS], int& turn, int wave0, int waves) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = SMALL ? sum16(v[k]) : sum64(v[k]);
-    if (!SMALL && waves > 1) {
+    for (int k = 0; k < K; ++k) v[k] = LANES == 16 ? sum16(v[k]) : LANES == 32 ? sum32(v[k]) : sum64(v[k]);
+    if (LANES == 64 && waves > 1) {
         float* at = sh[turn];
         turn ^= 1;
         if ((threadIdx.x & 63) == 0)
@@ -163,15 +167,15 @@ struct Kinds {
 //
 // A workgroup fills a CU (up to 1024 threads of up to 128 registers), with as many rows at a time as it holds: fewer partial sums
 // to write and add up than with a workgroup per row (N=4096 h=4096: 256 rows of them in place of 512).
-template <typename T, typename TD, typename TG, int C, bool SMALL, int PARTS>
+template <typename T, typename TD, typename TG, int C, int LANES, int PARTS>
 __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(BlockNormGrad p, ColumnSums s) {
     using K = Kinds<C, PARTS>;
     constexpr bool POST = K::POST, GATE = K::GATE, FULL = K::FULL;
     __shared__ float sh[2][K_ROW_SUMS];
     __shared__ float4 lds[K::SLOTS ? K::SLOTS * 2 * C * 1024 : 1];
     int turn = 0;
-    const int threads = SMALL ? 16 : s.threads, waves = threads >> 6;
-    const int group = SMALL ? threadIdx.x / 16 : __builtin_amdgcn_readfirstlane(threadIdx.x / threads);
+    const int threads = LANES < 64 ? LANES : s.threads, waves = threads >> 6;
+    const int group = LANES < 64 ? threadIdx.x / LANES : __builtin_amdgcn_readfirstlane(threadIdx.x / threads);
     const int t = threadIdx.x - group * threads, c0 = blockIdx.x * s.rows + group;
     const int64_t first = s.step == 1 ? (int64_t)c0 * s.each : c0;
     const int i0 = first < p.N ? (int)first : p.N, i1 = s.step == 1 && p.N - i0 > s.each ? i0 + s.each : p.N;
@@ -329,7 +333,7 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(BlockNormGrad p, C
                 if (live) add(K::DB, c, fresh, o);
             }
         }
-        row_sums<M, SMALL>(sums, sh, turn, group * waves, waves);
+        row_sums<M, LANES>(sums, sh, turn, group * waves, waves);
         const float mar = sums[0] * inv_h, ma = FULL && p.center ? sums[1] * inv_h : 0.f;
         float more[2] = {0.f, 0.f};
 #pragma unroll
@@ -379,7 +383,7 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(BlockNormGrad p, C
             }
         }
         if constexpr (POST) {
-            row_sums<M, SMALL>(more, sh, turn, group * waves, waves);
+            row_sums<M, LANES>(more, sh, turn, group * waves, waves);
             const float mky = more[0] * inv_h, mk = FULL && p.center ? more[1] * inv_h : 0.f;
 #pragma unroll
             for (int c = 0; c < C; ++c) {
@@ -448,9 +452,10 @@ static inline bool bwd_in_one_pass(int64_t h) { return h >= MIN_COLUMNS && h <= 
 template <typename T, typename TD, typename TG, int PARTS>
 static void launch_bwd_parts(const BlockNormGrad& p, const ColumnSums& s, hipStream_t st) {
     const dim3 grid(s.parts), block(s.rows * s.threads);
-    if (s.threads == 16) hipLaunchKernelGGL((block_norm_bwd_kernel<T, TD, TG, 1, true, PARTS>), grid, block, 0, st, p, s);
-    else if (p.h <= 8192) hipLaunchKernelGGL((block_norm_bwd_kernel<T, TD, TG, 1, false, PARTS>), grid, block, 0, st, p, s);
-    else hipLaunchKernelGGL((block_norm_bwd_kernel<T, TD, TG, 2, false, PARTS>), grid, block, 0, st, p, s);
+    if (s.threads == 16) hipLaunchKernelGGL((block_norm_bwd_kernel<T, TD, TG, 1, 16, PARTS>), grid, block, 0, st, p, s);
+    else if (s.threads == 32) hipLaunchKernelGGL((block_norm_bwd_kernel<T, TD, TG, 1, 32, PARTS>), grid, block, 0, st, p, s);
+    else if (p.h <= 8192) hipLaunchKernelGGL((block_norm_bwd_kernel<T, TD, TG, 1, 64, PARTS>), grid, block, 0, st, p, s);
+    else hipLaunchKernelGGL((block_norm_bwd_kernel<T, TD, TG, 2, 64, PARTS>), grid, block, 0, st, p, s);
 }
 template <typename T, typename TD, typename TG>
 static hipError_t launch_bwd_one_pass(const BlockNormGrad& p, const ColumnSums& s, hipStream_t st) {

@@ -131,7 +131,7 @@ __global__ __launch_bounds__(TR <= 64 ? 256 : TR) void block_norm_fwd_kernel(Blo
             for (int c = 0; c < C; ++c)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) s += e >= skip[c] ? v[c][e] : 0.f;
-            row_sums<1, TR == 16>(&s, sh, turn, 0, threads >> 6);
+            row_sums<1, TR == 16 ? 16 : 64>(&s, sh, turn, 0, threads >> 6);
             m.m = s / p.h;
         }
         s = 0.f;
@@ -142,7 +142,7 @@ __global__ __launch_bounds__(TR <= 64 ? 256 : TR) void block_norm_fwd_kernel(Blo
                 const float d = v[c][e] - m.m;
                 s += e >= skip[c] ? d * d : 0.f;
             }
-        row_sums<1, TR == 16>(&s, sh, turn, 0, threads >> 6);
+        row_sums<1, TR == 16 ? 16 : 64>(&s, sh, turn, 0, threads >> 6);
         m.rho = 1.f / sqrtf(s / p.h + p.eps);
         return m;
     };
@@ -357,8 +357,9 @@ ColumnSums cut(int64_t N, int64_t h, int64_t gate_rows) {
     int64_t parts;
     s.rows = 1;
     if (bwd_in_one_pass(h)) {
+        // (us, N=100000 bf16: h=100, 16 lanes 35.9, a wavefront 53.3; h=136 with everything, 32 lanes 55.3, a wavefront 69.7)
         const int64_t vectors = ceil_div(h, 8);
-        s.threads = h <= 128 ? 16 : (int)(ceil_div(h <= 8192 ? vectors : ceil_div(vectors, 2), 64) * 64);
+        s.threads = h <= 128 ? 16 : h <= 256 ? 32 : (int)(ceil_div(h <= 8192 ? vectors : ceil_div(vectors, 2), 64) * 64);
         s.rows = 1024 / s.threads;
         parts = CUS;
     } else {
@@ -397,8 +398,13 @@ hipError_t launch_block_norm_fwd(const BlockNorm& p, vp_dtype dt, hipStream_t st
         else hipLaunchKernelGGL((block_norm_fwd_kernel<float, TR, C, false>), grid, block, 0, st, p);                          \
         return hipGetLastError();                                                                                              \
     } while (0)
+    // As few threads per row as hold it with one or two vectors each: fewer steps in its sums, and no lane without columns (us, the
+    // choice against the next one: N=100000 h=100 bf16, 16 lanes 17.6, a wavefront 47.9; h=256, 16 lanes with two vectors 38.6, a
+    // wavefront 53.7; N=16384 h=600 layer norms, a wavefront 21.3, a workgroup 25.9; N=8192 h=2048, four wavefronts 27.5, one with four
+    // vectors 30.3; N=4096 h=4096, two vectors 26.3, one 26.8; N=2048 h=16384, 1024 threads with two 56, 512 with four 69).
     if (p.h >= MIN_COLUMNS && p.N <= 1 << 27) {      // (a launch has less than 2^32 threads)
         if (p.h <= 128) VP_FWD(16, 1, 256);
+        if (p.h <= 256) VP_FWD(16, 2, 256);
         if (p.h <= 512) VP_FWD(64, 1, 256);
         if (p.h <= 1024) VP_FWD(64, 2, 256);
         if (p.h <= 2048) VP_FWD(256, 1, (int)ceil_div(p.h, 512) * 64);

@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 F32, BF16 = torch.float32, torch.bfloat16
 # lengths from one element to rows that no workgroup holds, odd ones, powers of two and their neighbours
 SIZES = [(1, 1), (3, 7), (70, 8), (5, 63), (5, 64), (129, 65), (1, 128), (128, 256), (33, 511), (34, 1000), (17, 1001), (12, 1024),
-         (64, 2050), (7, 4096), (301, 4096), (9, 4104), (6, 8192), (3, 8200), (5, 12288), (4, 16384), (3, 16391), (2, 32768),
+         (64, 2050), (77, 200), (41, 129), (7, 4096), (301, 4096), (9, 4104), (6, 8192), (3, 8200), (5, 12288), (4, 16384), (3, 16391), (2, 32768),
          (2, 40001), (1, 70000), (1000, 40), (4099, 24)]
 
 
@@ -360,7 +360,7 @@ TYPES = [(F32, F32, F32), (BF16, F32, F32), (BF16, F32, BF16), (BF16, BF16, F32)
 
 @pytest.mark.parametrize("dtype,dH_type,grad", TYPES)
 @pytest.mark.parametrize("post,bias", list(itertools.product((False, True), repeat=2)))
-@pytest.mark.parametrize("N,h,gate", [(N, h, gate) for N, h in ((612, 90), (36, 1043), (612, 520), (36, 8203), (36, 4), (12, 260))
+@pytest.mark.parametrize("N,h,gate", [(N, h, gate) for N, h in ((612, 90), (612, 250), (36, 1043), (612, 520), (36, 8203), (36, 4), (12, 260))
                                       for gate in (0, 1, 4, 12, 36, 612) if not gate or N % gate == 0])
 def test_every_backward_kernel(N, h, post, gate, bias, dtype, dH_type, grad):
     """All types and parts at rows of lanes, wavefronts and a workgroup, two vectors per thread, and lengths below a vector; a
