@@ -115,8 +115,8 @@ __device__ __forceinline__ float sum64(float v) {
 }
 
 // Sums of K values over the threads of a row, a fixed tree: rows are held by 16 or 32 LANES, or (LANES = 64) by `waves` whole
-// wavefronts of the workgroup, the first of them `wave0`.  Several meet in LDS, in the half of `sh` that `turn` names (so that one barrier per
-// sum is enough: a thread that writes a half has passed the barrier behind which all others have read what it held).
+// wavefronts of the workgroup, the first of them `wave0`.  Several meet in LDS, in the half of `sh` that `turn` names (so that one
+// barrier per sum is enough: a thread that writes a half has passed the barrier behind which all others have read what it held).
 template <int K, int LANES>
 __device__ __forceinline__ void row_sums(float* v, float (*sh)[K_ROW_SUMS], int& turn, int wave0, int waves) {
 #pragma unroll
@@ -156,7 +156,8 @@ enum : int { NORM_POST = 1, NORM_GATE = 2, NORM_FULL = 4 };      // FULL: layer 
 template <int C, int PARTS>
 struct Kinds {
     static constexpr bool POST = PARTS & NORM_POST, GATE = PARTS & NORM_GATE, FULL = PARTS & NORM_FULL;
-    static constexpr int DW = 0, DWP = 1, DG = 1 + POST, DB = 1 + POST + GATE, DBP = DB + 1, COUNT = 1 + POST + GATE + FULL * (1 + POST);
+    static constexpr int DW = 0, DWP = 1, DG = 1 + POST, DB = 1 + POST + GATE, DBP = DB + 1;
+    static constexpr int COUNT = 1 + POST + GATE + FULL * (1 + POST);
     static constexpr int LDS0 = C == 1 ? 2 : 0, LDS1 = C == 1 ? COUNT : (COUNT < 2 ? COUNT : 2);      // kinds in LDS
     static constexpr bool in_registers(int kind) { return C == 1 ? kind < 2 : kind == 2; }
     static constexpr int SLOTS = LDS1 > LDS0 ? LDS1 - LDS0 : (C == 1 ? 1 : 0);
@@ -190,9 +191,13 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(BlockNormGrad p, C
     }
     float reg[2][8];      // of a kind (C = 1), of a vector (C = 2)
     auto in_reg = [&](int kind, int c) -> float* { return reg[C == 1 ? (kind < 2 ? kind : 0) : c]; };
-    auto slot = [&](int kind, int c, int half) -> float4& { return lds[(((kind - K::LDS0) * C + c) * 2 + half) * 1024 + threadIdx.x]; };
+    auto slot = [&](int kind, int c, int half) -> float4& {
+        return lds[(((kind - K::LDS0) * C + c) * 2 + half) * 1024 + threadIdx.x];
+    };
     auto matrix = [&](int kind) {
-        return kind == K::DW ? s.dw : POST && kind == K::DWP ? s.dw_post : GATE && kind == K::DG ? s.dgate : kind == K::DB ? s.db : s.db_post;
+        if (POST && kind == K::DWP) return s.dw_post;
+        if (GATE && kind == K::DG) return s.dgate;
+        return kind == K::DW ? s.dw : kind == K::DB ? s.db : s.db_post;
     };
 #pragma unroll
     for (int k = 0; k < 2; ++k)
