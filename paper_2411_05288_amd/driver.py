@@ -84,14 +84,17 @@ class BlockNormPlan:
 class GradientClipPlan:
     """The norm of many gradients together, and clipping by it: the gradients of all layers of a step, of fp32 or bf16, in place
     or into ``outs`` (tensors of their types and shapes, views of one flat buffer among them).  The plan keeps the tensors'
-    addresses: a gradient that moves needs a new plan.  A plan's calls share its workspace and ``norm``: they belong on one
-    stream, or one after the other."""
+    addresses: a gradient that moves needs a new plan.  A plan's calls share its workspace and ``norm`` (given, or the plan's
+    own): they belong on one stream, or one after the other."""
 
-    def __init__(self, grads: List[torch.Tensor], outs: Optional[List[torch.Tensor]] = None):
+    def __init__(self, grads: List[torch.Tensor], outs: Optional[List[torch.Tensor]] = None,
+                 norm: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
         self.arguments = B.GradientArguments(grads, outs)
         dev = self.arguments.grads[0].device if self.arguments.n else torch.device("cuda", torch.cuda.current_device())
-        self.norm = torch.empty((1,), dtype=torch.float32, device=dev)
-        self.workspace = torch.empty((B.vp_grad_workspace_bytes(self.arguments.n),), dtype=torch.uint8, device=dev)
+        self.norm = torch.empty((1,), dtype=torch.float32, device=dev) if norm is None else norm
+        if workspace is None:
+            workspace = torch.empty((B.vp_grad_workspace_bytes(self.arguments.n),), dtype=torch.uint8, device=dev)
+        self.workspace = workspace
 
     def covers(self, grads: List[torch.Tensor]) -> bool:
         """Whether it was made for exactly these tensors, and they are where they were."""
@@ -135,7 +138,7 @@ class OutputLayerPlan:
                  norm: Optional["BlockNormPlan"] = None):
         if (H is None) == (norm is None):
             raise B.VPError("either H or the norm that makes it")
-        self.norm, self.clip_plan = norm, None
+        self.norm, self.clip_plan, self.clip_norm, self.clip_workspaces = norm, None, None, []
         H = norm.H if H is None else H
         if algorithm not in (1, 2):
             raise B.VPError("algorithm must be 1 (two barriers) or 2 (one barrier)")
@@ -324,12 +327,18 @@ class OutputLayerPlan:
             self.norm.backward(self.dH, stream=stream)
 
     def clip_gradients(self, max_norm: float, others: Sequence[torch.Tensor] = (), stream=None) -> torch.Tensor:
-        """Clips in place by the norm of all gradients together, which it returns ([1], on the device)."""
+        """Clips in place by the norm of all gradients together, which it returns ([1], on the device, written by every call)."""
         grads = self.dW + (self.norm.parameter_gradients() if self.norm is not None else []) + list(others)
         if self.clip_plan is None or not self.clip_plan.covers(grads):
-            self.clip_plan = GradientClipPlan(grads)
+            # the norm and the workspaces stay where they are as long as this plan lives: a captured call has their addresses
+            if self.clip_norm is None:
+                self.clip_norm = torch.empty((1,), dtype=torch.float32, device=self.dH.device)
+            need = B.vp_grad_workspace_bytes(len(grads))
+            if not self.clip_workspaces or self.clip_workspaces[-1].numel() < need:
+                self.clip_workspaces.append(torch.empty((need,), dtype=torch.uint8, device=self.dH.device))
+            self.clip_plan = GradientClipPlan(grads, norm=self.clip_norm, workspace=self.clip_workspaces[-1])
         self.clip_plan.clip(max_norm, stream)
-        return self.clip_plan.norm
+        return self.clip_norm
 
     def step(self, stream=None) -> None:
         self.forward(stream)

@@ -338,3 +338,33 @@ def test_evaluation_with_a_norm_that_keeps_nothing():
     assert torch.equal(*losses) and norm.stats is None
     with pytest.raises(vp.VPError, match="train=False"):
         plan.backward()
+
+
+def test_a_captured_clipping_outlives_calls_with_other_gradients():
+    import paper_2411_05288_amd as vp
+    g = torch.Generator(device="cuda").manual_seed(6)
+    plan = vp.OutputLayerPlan(torch.randn(16, 32, generator=g, device="cuda"), [torch.randn(64, 32, generator=g, device="cuda")],
+                              torch.zeros(16, dtype=torch.int64, device="cuda"))
+    few = [torch.randn(100, generator=g, device="cuda") for _ in range(3)]
+    many = [torch.randn(50, generator=g, device="cuda") for _ in range(200)]
+    kept = [t.clone() for t in few]
+
+    def step():
+        for t, k in zip(few, kept):
+            t.copy_(k)
+        plan.step()
+        return plan.clip_gradients(0.1, few)
+    total = step().clone()
+    expected = [t.clone() for t in few + plan.dW]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        other = plan.clip_gradients(1e9, many)      # a larger list, another plan and workspace
+        assert float(other) > float(total)
+        junk = [torch.full((1 << 14,), float("nan"), device="cuda") for _ in range(20)]      # what was freed is written by others
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(plan.clip_norm, total)
+        assert all(torch.equal(a, b) for a, b in zip(few + plan.dW, expected))
+        assert all(bool(torch.isnan(t).all()) for t in junk)
