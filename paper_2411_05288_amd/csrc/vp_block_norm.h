@@ -152,18 +152,18 @@ enum : int { NORM_POST = 1, NORM_GATE = 2, NORM_FULL = 4 };      // FULL: layer 
 
 // Where the sums over tokens of a thread's columns are kept: kind 0 is dw, the others are numbered as they are there.  C = 1
 // (up to 8192 columns): two kinds in registers, the others in LDS.  C = 2 (up to 16384): two in LDS, one in registers, the others
-// in the workgroup's row of the partial matrices, which the L2 holds.
+// in the workgroup's row of the partial matrices, which the L2 holds.  C = 4 (up to 32768): one in LDS, the others there.
 template <int C, int PARTS>
 struct Kinds {
     static constexpr bool POST = PARTS & NORM_POST, GATE = PARTS & NORM_GATE, FULL = PARTS & NORM_FULL;
     static constexpr int DW = 0, DWP = 1, DG = 1 + POST, DB = 1 + POST + GATE, DBP = DB + 1;
     static constexpr int COUNT = 1 + POST + GATE + FULL * (1 + POST);
-    static constexpr int LDS0 = C == 1 ? 2 : 0, LDS1 = C == 1 ? COUNT : (COUNT < 2 ? COUNT : 2);      // kinds in LDS
-    static constexpr bool in_registers(int kind) { return C == 1 ? kind < 2 : kind == 2; }
+    static constexpr int LDS0 = C == 1 ? 2 : 0, LDS1 = C == 1 ? COUNT : C == 4 || COUNT < 2 ? 1 : 2;      // kinds in LDS
+    static constexpr bool in_registers(int kind) { return C == 1 ? kind < 2 : C == 2 && kind == 2; }
     static constexpr int SLOTS = LDS1 > LDS0 ? LDS1 - LDS0 : (C == 1 ? 1 : 0);
 };
 
-// Rows of 8 to 8192 C columns in one pass: a row's values stay in registers between the sums over it and dx and dy, and a thread's
+// Rows of 8 to 8192 C columns in one pass (N=512 h=32768 bf16: 112 us, with a launch for each step 290): a row's values stay in registers between the sums over it and dx and dy, and a thread's
 // columns are the same in every row of its range, so the sums over tokens stay on the chip too.
 //
 // A workgroup fills a CU (up to 1024 threads of up to 128 registers), with as many rows at a time as it holds: fewer partial sums
@@ -189,7 +189,7 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(BlockNormGrad p, C
         j[c] = cols.j;
         skip[c] = cols.skip;
     }
-    float reg[2][8];      // of a kind (C = 1), of a vector (C = 2)
+    float reg[C == 4 ? 4 : 2][8];      // of a kind (C = 1), of a vector (C = 2), nothing (C = 4)
     auto in_reg = [&](int kind, int c) -> float* { return reg[C == 1 ? (kind < 2 ? kind : 0) : c]; };
     auto slot = [&](int kind, int c, int half) -> float4& {
         return lds[(((kind - K::LDS0) * C + c) * 2 + half) * 1024 + threadIdx.x];
@@ -236,7 +236,7 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(BlockNormGrad p, C
             keep(kind, c, v);
         }
     };
-    // What is read of a row.  C = 1: once, and kept in registers from the first sums to the last.  C = 2: again in every step, from
+    // What is read of a row.  C = 1: once, and kept in registers from the first sums to the last.  C > 1: again in every step, from
     // the caches (two vectors of everything at once do not fit: N=2048 h=16384, kept, 124 us for bf16 RMS norms, 215 for fp32 ones
     // and 270 with everything; read again, 127, 196 and 257).
     struct Values {
@@ -441,7 +441,7 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(BlockNormGrad p, C
         const float* from = reinterpret_cast<const float*>(lds + (C == 1 && k < 2 ? 0 : (k - K::LDS0) * C * 2 * 1024));
         for (int col = threadIdx.x; col < p.h; col += blockDim.x) {
             int vec = col >> 3;
-            const int e = col - Columns(vec, p.h).j, c = vec >= threads ? 1 : 0;
+            const int e = col - Columns(vec, p.h).j, c = C == 1 ? 0 : vec / threads;
             vec -= c * threads;
             float q = 0.f;
             for (int r = 0; r < s.rows; ++r) q += from[((c * 2 + (e >> 2)) * 1024 + r * threads + vec) * 4 + (e & 3)];
@@ -451,7 +451,8 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(BlockNormGrad p, C
 }
 
 // Whether rows of h columns are held by threads in the backward pass.
-constexpr int MIN_COLUMNS = 8, BWD_MAX_COLUMNS = 16384;
+constexpr int MIN_COLUMNS = 8, BWD_MAX_COLUMNS = 32768;
+static inline int bwd_vectors(int64_t h) { return h <= 8192 ? 1 : h <= 16384 ? 2 : 4; }      // of a thread
 static inline bool bwd_in_one_pass(int64_t h) { return h >= MIN_COLUMNS && h <= BWD_MAX_COLUMNS; }
 
 template <typename T, typename TD, typename TG, int PARTS>
@@ -459,8 +460,9 @@ static void launch_bwd_parts(const BlockNormGrad& p, const ColumnSums& s, hipStr
     const dim3 grid(s.parts), block(s.rows * s.threads);
     if (s.threads == 16) hipLaunchKernelGGL((block_norm_bwd_kernel<T, TD, TG, 1, 16, PARTS>), grid, block, 0, st, p, s);
     else if (s.threads == 32) hipLaunchKernelGGL((block_norm_bwd_kernel<T, TD, TG, 1, 32, PARTS>), grid, block, 0, st, p, s);
-    else if (p.h <= 8192) hipLaunchKernelGGL((block_norm_bwd_kernel<T, TD, TG, 1, 64, PARTS>), grid, block, 0, st, p, s);
-    else hipLaunchKernelGGL((block_norm_bwd_kernel<T, TD, TG, 2, 64, PARTS>), grid, block, 0, st, p, s);
+    else if (bwd_vectors(p.h) == 1) hipLaunchKernelGGL((block_norm_bwd_kernel<T, TD, TG, 1, 64, PARTS>), grid, block, 0, st, p, s);
+    else if (bwd_vectors(p.h) == 2) hipLaunchKernelGGL((block_norm_bwd_kernel<T, TD, TG, 2, 64, PARTS>), grid, block, 0, st, p, s);
+    else hipLaunchKernelGGL((block_norm_bwd_kernel<T, TD, TG, 4, 64, PARTS>), grid, block, 0, st, p, s);
 }
 template <typename T, typename TD, typename TG>
 static hipError_t launch_bwd_one_pass(const BlockNormGrad& p, const ColumnSums& s, hipStream_t st) {

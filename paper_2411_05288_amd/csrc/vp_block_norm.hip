@@ -9,7 +9,7 @@ namespace vp {
 
 namespace {
 
-// Sums of K values over the workgroup (1024 threads), a fixed tree; sh: K * 16 floats.
+// Sums of K values over the workgroup (up to 16 wavefronts), a fixed tree; sh: K * 16 floats.
 template <int K>
 __device__ __forceinline__ void block_sums(float* v, float* sh) {
 #pragma unroll
@@ -24,8 +24,7 @@ __device__ __forceinline__ void block_sums(float* v, float* sh) {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         float s = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s += sh[k * 16 + i];
+        for (int i = 0; i < (int)(blockDim.x >> 6); ++i) s += sh[k * 16 + i];
         v[k] = s;
     }
 }
@@ -40,12 +39,12 @@ __device__ __forceinline__ Normed statistics(F f, int h, int center, float eps, 
     float s;
     if (center) {
         s = 0.f;
-        for (int j = threadIdx.x; j < h; j += 1024) s += f(j);
+        for (int j = threadIdx.x; j < h; j += blockDim.x) s += f(j);
         block_sums<1>(&s, sh);
         n.m = s / h;
     }
     s = 0.f;
-    for (int j = threadIdx.x; j < h; j += 1024) {
+    for (int j = threadIdx.x; j < h; j += blockDim.x) {
         const float d = f(j) - n.m;
         s += d * d;
     }
@@ -72,7 +71,7 @@ __global__ __launch_bounds__(1024) void block_norm_fwd_long_kernel(BlockNorm p) 
             return v + p.scale * ld_or(gate, j, 1.f) * u;
         };
         const Normed n = statistics(sum, p.h, p.center, p.eps, sh);
-        for (int j = threadIdx.x; j < p.h; j += 1024) {
+        for (int j = threadIdx.x; j < p.h; j += blockDim.x) {
             const float v = sum(j);
             if (p.r) put((T*)p.r + row + j, v);
             put((T*)p.H + row + j, (v - n.m) * n.rho * ld_or((const T*)p.w, j, 1.f) + ld_or((const T*)p.b, j, 0.f));
@@ -223,7 +222,7 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_means_kernel(BlockNormGra
     for (int64_t i = blockIdx.x; i < p.N; i += gridDim.x) {
         const Row<T, TD, TG> q(p, i);
         float s[2] = {0.f, 0.f}, c[2] = {0.f, 0.f};
-        for (int j = threadIdx.x; j < p.h; j += 1024) {
+        for (int j = threadIdx.x; j < p.h; j += blockDim.x) {
             const float a = q.a(p, j);
             s[0] += a;
             s[1] += a * q.rh(j);
@@ -231,7 +230,7 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_means_kernel(BlockNormGra
         block_sums<2>(s, sh);
         const float ma = p.center ? s[0] / p.h : 0.f, mar = s[1] / p.h;
         if (p.post) {
-            for (int j = threadIdx.x; j < p.h; j += 1024) {
+            for (int j = threadIdx.x; j < p.h; j += blockDim.x) {
                 const float v = q.d(p, j, q.g(p, j, ma, mar)) * ld_or((const T*)p.w_post, j, 1.f);
                 c[0] += v;
                 c[1] += v * q.yh(j);
@@ -289,7 +288,7 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_rows_kernel(BlockNormGrad
         const Row<T, TD, TG> q(p, i);
         const float4 m = means[i];
         TG *dx = (TG*)p.dx + (size_t)i * p.h, *dy = p.dy ? (TG*)p.dy + (size_t)i * p.h : nullptr;
-        for (int j = threadIdx.x; j < p.h; j += 1024) {
+        for (int j = threadIdx.x; j < p.h; j += blockDim.x) {
             const float g = q.g(p, j, m.x, m.y);
             if (dy) {
                 float d = q.d(p, j, g);
@@ -361,7 +360,7 @@ ColumnSums cut(int64_t N, int64_t h, int64_t gate_rows) {
     if (bwd_in_one_pass(h)) {
         // (us, N=100000 bf16: h=100, 16 lanes 35.9, a wavefront 53.3; h=136 with everything, 32 lanes 55.3, a wavefront 69.7)
         const int64_t vectors = ceil_div(h, 8);
-        s.threads = h <= 128 ? 16 : h <= 256 ? 32 : (int)(ceil_div(h <= 8192 ? vectors : ceil_div(vectors, 2), 64) * 64);
+        s.threads = h <= 128 ? 16 : h <= 256 ? 32 : (int)(ceil_div(ceil_div(vectors, bwd_vectors(h)), 64) * 64);
         s.rows = 1024 / s.threads;
         parts = CUS;
     } else {
@@ -384,6 +383,8 @@ ColumnSums cut(int64_t N, int64_t h, int64_t gate_rows) {
 }
 
 constexpr int MAX_ROW_BLOCKS = 1 << 16;
+// Threads of a row of any length: a wavefront where it is shorter than a vector (N=100000 h=4: 50 us, with 1024 threads 895).
+int long_threads(int64_t h) { return h < MIN_COLUMNS ? 64 : 1024; }
 
 }  // namespace
 
@@ -404,7 +405,7 @@ hipError_t launch_block_norm_fwd(const BlockNorm& p, vp_dtype dt, hipStream_t st
     // the choice against the next one: N=100000 h=100 bf16, 16 lanes 17.6, a wavefront 47.9; h=256, 16 lanes with two vectors
     // 38.6, a wavefront 53.7; N=16384 h=600 layer norms, a wavefront 21.3, a workgroup 25.9; N=8192 h=2048, four wavefronts
     // 27.5, one with four vectors 30.3; N=4096 h=4096, two vectors 26.3, one 26.8; N=2048 h=16384, 1024 threads with two 56, 512
-    // with four 69).
+    // with four 69; N=512 h=32768, 1024 with four 31, a row that is read again for every sum 126).
     if (p.h >= MIN_COLUMNS && p.N <= 1 << 27) {      // (a launch has less than 2^32 threads)
         if (p.h <= 128) VP_FWD(16, 1, 256);
         if (p.h <= 256) VP_FWD(16, 2, 256);
@@ -413,11 +414,12 @@ hipError_t launch_block_norm_fwd(const BlockNorm& p, vp_dtype dt, hipStream_t st
         if (p.h <= 2048) VP_FWD(256, 1, (int)ceil_div(p.h, 512) * 64);
         if (p.h <= 8192) VP_FWD(512, 2, (int)ceil_div(p.h, 1024) * 64);
         if (p.h <= 16384) VP_FWD(1024, 2, (int)ceil_div(p.h, 1024) * 64);
+        if (p.h <= 32768) VP_FWD(1024, 4, (int)ceil_div(p.h, 2048) * 64);
     }
 #undef VP_FWD
     const int blocks = p.N < MAX_ROW_BLOCKS ? p.N : MAX_ROW_BLOCKS;
-    if (bf16) hipLaunchKernelGGL(block_norm_fwd_long_kernel<u16>, dim3(blocks), dim3(1024), 0, st, p);
-    else hipLaunchKernelGGL(block_norm_fwd_long_kernel<float>, dim3(blocks), dim3(1024), 0, st, p);
+    if (bf16) hipLaunchKernelGGL(block_norm_fwd_long_kernel<u16>, dim3(blocks), dim3(long_threads(p.h)), 0, st, p);
+    else hipLaunchKernelGGL(block_norm_fwd_long_kernel<float>, dim3(blocks), dim3(long_threads(p.h)), 0, st, p);
     return hipGetLastError();
 }
 
@@ -433,12 +435,12 @@ size_t block_norm_bwd_workspace(int64_t N, int64_t h, int64_t gate_rows, bool po
 template <typename T, typename TD, typename TG>
 static hipError_t launch_bwd_long(const BlockNormGrad& p, const ColumnSums& s, float4* means, hipStream_t st) {
     const int blocks = p.N < MAX_ROW_BLOCKS ? p.N : MAX_ROW_BLOCKS;
-    hipLaunchKernelGGL((block_norm_bwd_means_kernel<T, TD, TG>), dim3(blocks), dim3(1024), 0, st, p, means);
+    hipLaunchKernelGGL((block_norm_bwd_means_kernel<T, TD, TG>), dim3(blocks), dim3(long_threads(p.h)), 0, st, p, means);
     // (before dx is written: it may be dr)
     if (p.dw || p.db || p.dw_post || p.db_post || p.dgate)
         hipLaunchKernelGGL((block_norm_bwd_columns_kernel<T, TD, TG>), dim3((unsigned)ceil_div(p.h, 256), s.parts), dim3(256), 0, st,
                            p, means, s);
-    hipLaunchKernelGGL((block_norm_bwd_rows_kernel<T, TD, TG>), dim3(blocks), dim3(1024), 0, st, p, means);
+    hipLaunchKernelGGL((block_norm_bwd_rows_kernel<T, TD, TG>), dim3(blocks), dim3(long_threads(p.h)), 0, st, p, means);
     return hipGetLastError();
 }
 

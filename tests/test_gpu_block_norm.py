@@ -360,7 +360,7 @@ TYPES = [(F32, F32, F32), (BF16, F32, F32), (BF16, F32, BF16), (BF16, BF16, F32)
 
 @pytest.mark.parametrize("dtype,dH_type,grad", TYPES)
 @pytest.mark.parametrize("post,bias", list(itertools.product((False, True), repeat=2)))
-@pytest.mark.parametrize("N,h,gate", [(N, h, gate) for N, h in ((612, 90), (612, 250), (36, 1043), (612, 520), (36, 8203), (36, 4), (12, 260))
+@pytest.mark.parametrize("N,h,gate", [(N, h, gate) for N, h in ((612, 90), (612, 250), (36, 1043), (612, 520), (36, 8203), (36, 4), (12, 260), (12, 18437), (12, 33000))
                                       for gate in (0, 1, 4, 12, 36, 612) if not gate or N % gate == 0])
 def test_every_backward_kernel(N, h, post, gate, bias, dtype, dH_type, grad):
     """All types and parts at rows of lanes, wavefronts and a workgroup, two vectors per thread, and lengths below a vector; a
