@@ -163,8 +163,9 @@ struct Kinds {
     static constexpr int SLOTS = LDS1 > LDS0 ? LDS1 - LDS0 : (C == 1 ? 1 : 0);
 };
 
-// Rows of 8 to 8192 C columns in one pass (N=512 h=32768 bf16: 112 us, with a launch for each step 290): a row's values stay in registers between the sums over it and dx and dy, and a thread's
-// columns are the same in every row of its range, so the sums over tokens stay on the chip too.
+// Rows of 8 to 8192 C columns in one pass (N=512 h=32768 bf16: 112 us, with a launch for each step 290): a row's values stay on
+// the chip between the sums over it and dx and dy, and a thread's columns are the same in every row of its range, so the sums
+// over tokens stay there too.
 //
 // A workgroup fills a CU (up to 1024 threads of up to 128 registers), with as many rows at a time as it holds: fewer partial sums
 // to write and add up than with a workgroup per row (N=4096 h=4096: 256 rows of them in place of 512).
