@@ -109,7 +109,7 @@ def test_norm_alone(N, h, dtype, center):
     ref.check("dw", dw, *expected["dw"])
 
 
-@pytest.mark.parametrize("N,h", [(9, 1000), (3, 4096), (2, 40000)])
+@pytest.mark.parametrize("N,h", [(9, 1000), (3, 4096), (2, 40000), (700, 77), (700, 205), (600, 1001), (300, 4099), (40, 9001), (20, 18437), (50, 5)])
 def test_in_place(N, h):
     import paper_2411_05288_amd as vp
     s = inputs(N, h, BF16, True, 1, True, 4)
