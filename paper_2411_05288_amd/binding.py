@@ -566,7 +566,8 @@ def vp_block_norm_fwd(x, y, H, *, r=None, stats=None, gate=None, w=None, b=None,
     if _HOST is not None:
         st = _HOST.block_norm_fwd(_ADDRESS["vp_block_norm_fwd"], x, y, H, r, stats, gate, w, b, w_post, b_post, scale, eps,
                                   _norm_flags(post, center), stream)
-        if st == 0:
+        if st is not None:      # the call was made: whatever it returned, not once more
+            _check(st, "vp_block_norm_fwd")
             return
     if x.dim() != 2:
         raise VPError("x must be [N, h]")
@@ -600,7 +601,8 @@ def vp_block_norm_bwd(dH, r, y, stats, *, dx, dy=None, dr=None, gate=None, w=Non
     if _HOST is not None:
         st = _HOST.block_norm_bwd(_ADDRESS["vp_block_norm_bwd"], dH, r, y, stats, dx, dy, dr, gate, w, w_post, b_post, scale,
                                   _norm_flags(post, center), dgate, dw, db, dw_post, db_post, workspace, stream)
-        if st == 0:
+        if st is not None:      # the call was made: whatever it returned, not once more
+            _check(st, "vp_block_norm_bwd")
             return
     if r.dim() != 2:
         raise VPError("r must be [N, h]")
