@@ -625,8 +625,9 @@ def vp_block_norm_bwd(dH, r, y, stats, *, dx, dy=None, dr=None, gate=None, w=Non
 
 
 class GradientArguments:
-    """The host arrays that the calls over many gradients take.  It holds raw addresses: the tensors have to live, and to stay
-    where they are, as long as it is used (it keeps them alive).  outs: where the clipped gradients go, None = in place."""
+    """The host arrays that the calls over many gradients take: addresses and sizes of the tensors, which it keeps alive.  A
+    tensor that moved or changed its size or type since is refused by every call with these arguments (a captured call has the
+    addresses for good).  outs: where the clipped gradients go, None = in place."""
 
     def __init__(self, grads, outs=None):
         self.grads, self.outs = list(grads), None if outs is None else list(outs)
@@ -656,8 +657,24 @@ class GradientArguments:
             else:
                 read = max(read, start + size)
 
+    def unchanged(self, outs: bool = True) -> bool:
+        """Whether the tensors (with their outputs) are where and what they were when this was made."""
+        return _unchanged(self.grads, self.ptrs, self.counts, self.dts) and (
+            not outs or self.outs is None or _unchanged(self.outs, self.out_ptrs, self.counts, self.dts))
+
+
+def _unchanged(ts, ptrs, counts, dts) -> bool:
+    if _HOST is not None and _HOST.unchanged(ts, ptrs, counts, dts):
+        return True
+    kinds = {VP_F32: (torch.float32,), VP_BF16: _BF16_LIKE}
+    return len(ts) == len(ptrs) and all(
+        t.numel() == n and t.dtype in kinds[d] and t.is_contiguous() and (n == 0 or t.data_ptr() == p)
+        for t, p, n, d in zip(ts, ptrs, counts, dts))
+
 
 def _grad_call(name: str, a, norm, workspace, stream, max_norm=None):
+    if not a.unchanged(outs=max_norm is not None):
+        raise VPError("%s: a tensor has moved or changed its size or type since the arguments were made" % name)
     if max_norm is not None and a.overlap:
         raise VPError("%s: an output shares memory with another one or with another gradient" % name)
     lib = load_library()

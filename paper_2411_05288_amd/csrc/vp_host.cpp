@@ -43,6 +43,10 @@ bool shape_ok(const at::Tensor& t, PyObject* shape) {
     return true;
 }
 
+// bf16 data may come as bit patterns.
+bool bf16_like(at::ScalarType t) { return t == at::kBFloat16 || t == at::kShort || t == at::kUInt16; }
+int vp_dtype_of(at::ScalarType t) { return t == at::kFloat ? 0 : bf16_like(t) ? 1 : -1; }
+
 // The address of the tensor's first element in `out`, if it passes all checks.
 bool address(PyObject* o, PyObject* dtypes, PyObject* shape, uint64_t& out) {
     if (!THPVariable_CheckExact(o)) return false;
@@ -115,6 +119,42 @@ PyObject* on_current_device(PyObject*, PyObject* ts) {
     Py_RETURN_TRUE;
 }
 
+// The memory of an object of the buffer protocol (a ctypes array).
+struct Buffer {
+    Py_buffer view{};
+    explicit Buffer(PyObject* o) {
+        if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) PyErr_Clear();
+    }
+    ~Buffer() { PyBuffer_Release(&view); }
+    template <typename T>
+    const T* of(Py_ssize_t n) const { return view.buf && view.len == n * (Py_ssize_t)sizeof(T) ? static_cast<const T*>(view.buf) : nullptr; }
+};
+
+// unchanged(list of tensors, their addresses, numbers of elements and vp_dtypes as arrays) -> True, where they still are as the
+// arrays say (13 ns a tensor)
+PyObject* unchanged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 4 || !PyList_Check(a[0])) Py_RETURN_NONE;
+    const Py_ssize_t k = PyList_GET_SIZE(a[0]);
+    if (k == 0) Py_RETURN_NONE;
+    const Buffer buffers[3] = {Buffer(a[1]), Buffer(a[2]), Buffer(a[3])};
+    const uint64_t* ptrs = buffers[0].of<uint64_t>(k);
+    const int64_t* counts = buffers[1].of<int64_t>(k);
+    const int32_t* dts = buffers[2].of<int32_t>(k);
+    if (!ptrs || !counts || !dts) Py_RETURN_NONE;
+    try {
+        for (Py_ssize_t i = 0; i < k; ++i) {
+            PyObject* o = PyList_GET_ITEM(a[0], i);
+            if (!THPVariable_CheckExact(o)) Py_RETURN_NONE;
+            const at::Tensor& t = THPVariable_Unpack(o);
+            if (!t.defined() || t.numel() != counts[i] || vp_dtype_of(t.scalar_type()) != dts[i] || !t.is_contiguous()) Py_RETURN_NONE;
+            if (counts[i] && reinterpret_cast<uint64_t>(t.data_ptr()) != ptrs[i]) Py_RETURN_NONE;
+        }
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    Py_RETURN_TRUE;
+}
+
 // stream() -> int: the current stream of the current device
 PyObject* stream(PyObject*, PyObject*) {
     try {
@@ -132,16 +172,11 @@ struct Call {
     at::DeviceIndex here = c10::hip::current_device();
     bool ok = true;
 
-    static bool bf16_like(at::ScalarType t) { return t == at::kBFloat16 || t == at::kShort || t == at::kUInt16; }
     // vp_dtype of a tensor
     int dtype(PyObject* o) {
-        if (THPVariable_CheckExact(o)) {
-            const at::ScalarType t = THPVariable_Unpack(o).scalar_type();
-            if (t == at::kFloat) return 0;
-            if (bf16_like(t)) return 1;
-        }
-        ok = false;
-        return 0;
+        const int dt = THPVariable_CheckExact(o) ? vp_dtype_of(THPVariable_Unpack(o).scalar_type()) : -1;
+        if (dt < 0) ok = false;
+        return dt;
     }
     // the address of a tensor of the shape and type; None is null
     void* at(PyObject* o, int dtype, std::initializer_list<int64_t> shape) {
@@ -261,6 +296,7 @@ PyMethodDef methods[] = {
     {"ptrs", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(ptrs)), METH_FASTCALL, nullptr},
     {"same_shapes", same_shapes, METH_O, nullptr},
     {"on_current_device", on_current_device, METH_O, nullptr},
+    {"unchanged", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(unchanged)), METH_FASTCALL, nullptr},
     {"stream", stream, METH_NOARGS, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

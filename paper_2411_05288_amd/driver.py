@@ -83,9 +83,10 @@ class BlockNormPlan:
 
 class GradientClipPlan:
     """The norm of many gradients together, and clipping by it: the gradients of all layers of a step, of fp32 or bf16, in place
-    or into ``outs`` (tensors of their types and shapes, views of one flat buffer among them).  The plan keeps the tensors'
-    addresses: a gradient that moves needs a new plan.  A plan's calls share its workspace and ``norm`` (given, or the plan's
-    own): they belong on one stream, or one after the other."""
+    or into ``outs`` (tensors of their types and shapes, views of one flat buffer among them).  The plan keeps the tensors and
+    their addresses: gradients that are other tensors in the next step need a new plan (``covers``), and a tensor that moved or
+    changed its size or type is refused.  A plan's calls share its workspace and ``norm`` (given, or the plan's own): they belong
+    on one stream, or one after the other."""
 
     def __init__(self, grads: List[torch.Tensor], outs: Optional[List[torch.Tensor]] = None,
                  norm: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
@@ -97,9 +98,9 @@ class GradientClipPlan:
         self.workspace = workspace
 
     def covers(self, grads: List[torch.Tensor]) -> bool:
-        """Whether it was made for exactly these tensors, and they are where they were."""
+        """Whether it was made for exactly these tensors, and they are where and what they were."""
         a = self.arguments
-        return a.n == len(grads) and all(g is mine and (g.data_ptr() or None) == p for g, mine, p in zip(grads, a.grads, a.ptrs))
+        return a.n == len(grads) and all(g is mine for g, mine in zip(grads, a.grads)) and a.unchanged()
 
     def compute_norm(self, stream=None) -> None:
         B.vp_grad_norm(self.arguments, self.norm, self.workspace, stream)

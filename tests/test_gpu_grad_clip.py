@@ -368,3 +368,29 @@ def test_a_captured_clipping_outlives_calls_with_other_gradients():
         assert torch.equal(plan.clip_norm, total)
         assert all(torch.equal(a, b) for a, b in zip(few + plan.dW, expected))
         assert all(bool(torch.isnan(t).all()) for t in junk)
+
+
+def test_plan_notices_gradients_that_changed_where_they_are():
+    """A shorter view or another type at the same address: what lies behind is not touched, and the list is made anew."""
+    import paper_2411_05288_amd as vp
+    plan = vp.OutputLayerPlan(torch.randn(16, 32, device="cuda"), [torch.randn(64, 32, device="cuda")],
+                              torch.zeros(16, dtype=torch.int64, device="cuda"))
+    plan.step()
+    whole = torch.full((400,), 3.0, device="cuda")
+    other = whole[:300]
+    kept = vp.GradientClipPlan([other])
+    plan.clip_gradients(1e6, [other])
+    first = plan.clip_plan
+    other.data = other.data[:100]
+    total = plan.clip_gradients(1e-3, [other])
+    assert plan.clip_plan is not first and abs(exact_norm([other, *plan.dW]) - 1e-3) <= 1e-8 and float(total) > 30
+    assert bool((whole[100:] == 3).all())
+    other.data = other.data.view(BF16)[:100]
+    with pytest.raises(vp.VPError, match="since the arguments were made"):
+        kept.clip(1e-3)
+    with pytest.raises(vp.VPError, match="since the arguments were made"):
+        kept.compute_norm()
+    other.fill_(2.0)
+    total = plan.clip_gradients(1.0, [other])
+    assert plan.clip_plan.arguments.dts[-1] == vp.VP_BF16 and abs(float(total) - 20) <= 1e-4      # 10 * 2 and what is left of dW
+    assert bool((whole[100:] == 3).all())

@@ -66,3 +66,76 @@ def test_a_norm_call_that_was_not_made_is_made_with_the_checks_in_python(library
     vp.vp_block_norm_fwd(x, None, y, stats=stats)
     vp.vp_block_norm_bwd(x, x, None, stats, dx=y, workspace=torch.zeros(1 << 16, dtype=torch.uint8))
     assert [name for name, _ in library.calls] == ["vp_block_norm_fwd", "vp_block_norm_bwd"]
+
+
+def changes():
+    """(name, what a program may do to a tensor of 100 fp32 elements that the arguments of a call were made of)"""
+    def moved(t):
+        t.data = t.data.clone()
+
+    def shorter(t):      # the same address: the old number of elements would reach into what lies behind
+        t.data = t.data[:50]
+
+    def longer(t):
+        t.data = t.data.as_strided((120,), (1,))
+
+    def resized(t):
+        t.resize_(99)
+
+    def other_type(t):
+        t.data = t.data.view(torch.bfloat16)[:100]
+
+    def strided(t):
+        t.data = t.data.view(10, 10).t()
+
+    def freed(t):
+        t.untyped_storage().resize_(0)
+    return [moved, shorter, longer, resized, other_type, strided, freed]
+
+
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("change", changes(), ids=lambda f: f.__name__)
+@pytest.mark.parametrize("of_outs", [False, True])
+def test_tensors_that_changed_are_not_written(library, monkeypatch, native, change, of_outs):
+    """The arguments hold addresses and numbers of elements: what no longer fits them is refused before anything is called."""
+    import paper_2411_05288_amd as vp
+    import paper_2411_05288_amd.binding as B
+    host = B._load_host(B.host_path()) if native else None
+    if native and host is None:
+        pytest.skip("_vphost.so is not built for this PyTorch")
+    monkeypatch.setattr(B, "_HOST", host)
+    ws, norm = torch.zeros(1 << 16, dtype=torch.uint8), torch.zeros(1)
+    grads = [torch.zeros(300), torch.zeros(400)[:100], torch.zeros(0)]
+    outs = [torch.zeros(300), torch.zeros(400)[:100], torch.zeros(0)]
+    plan = vp.GradientClipPlan(grads, outs, norm=norm, workspace=ws)
+    calls = [plan.compute_norm, lambda: plan.clip(1.0), lambda: plan.scale(1.0)]
+    for call in calls:
+        call()
+    assert plan.covers(grads) and [name for name, _ in library.calls] == ["vp_grad_norm", "vp_grad_clip", "vp_grad_scale"]
+    library.calls.clear()
+    change((outs if of_outs else grads)[1])
+    assert not plan.covers(grads)
+    for call in calls[1 if of_outs else 0:]:
+        with pytest.raises(vp.VPError, match="since the arguments were made"):
+            call()
+    assert library.calls == []
+    vp.GradientClipPlan(grads[:1], outs[:1], norm=norm, workspace=ws).clip(1.0)      # the others are as they were
+    assert len(library.calls) == 1
+
+
+@pytest.mark.parametrize("change", changes()[:3], ids=lambda f: f.__name__)
+def test_clip_gradients_of_a_changed_tensor(library, monkeypatch, change):
+    """The kept list of gradients is made anew for a gradient that is another one at the same address."""
+    import paper_2411_05288_amd as vp
+    W, other = [torch.zeros(16, 8)], torch.zeros(400)[:100]
+    monkeypatch.setattr(vp.OutputLayerPlan, "__init__", lambda self: None)
+    plan = vp.OutputLayerPlan()
+    plan.dW, plan.norm, plan.dH = W, None, torch.zeros(4, 8)
+    plan.clip_plan, plan.clip_norm, plan.clip_workspaces = None, None, []
+    monkeypatch.setattr("paper_2411_05288_amd.binding.vp_grad_workspace_bytes", lambda n: 1 << 16)
+    plan.clip_gradients(1.0, [other])
+    change(other)
+    plan.clip_gradients(1.0, [other])
+    counts = [list(args[1]) for _, args in library.calls]
+    assert counts == [[128, 100], [128, other.numel()]]
+    assert library.calls[1][1][0][1] == other.data_ptr()
