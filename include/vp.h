@@ -41,7 +41,7 @@ extern "C" {
 
 typedef enum {
     VP_OK = 0,
-    VP_ERR_INVALID_ARG = 1, /* null pointer, non-positive size, bad enum, misaligned pointer */
+    VP_ERR_INVALID_ARG = 1, /* null pointer, non-positive size, bad enum, misaligned pointer, shared memory */
     VP_ERR_UNSUPPORTED = 2, /* valid request outside the implemented size limits */
     VP_ERR_WORKSPACE = 3,   /* workspace NULL or smaller than vp_workspace_bytes() */
     VP_ERR_DEVICE = 4       /* the HIP runtime reported an error at launch */
@@ -344,7 +344,8 @@ vp_status vp_block_norm_bwd(const void* dH, vp_dtype dH_dt, const void* dr, cons
  * Gradients may start at any element (4 bytes with VP_F32, 2 with VP_BF16).
  *     norm[0] = sqrt( sum over all elements of all gradients of g^2 )
  * Squares are formed and summed in fp64, in a fixed order: none over- or underflows, results repeat bit for bit.
- *   norm [1] : out, fp32.  The workspace has vp_grad_workspace_bytes(n) bytes ((size_t)-1 for n < 0).
+ *   norm [1] : out, fp32.  The workspace has vp_grad_workspace_bytes(n) bytes ((size_t)-1 for n < 0).  Norm and workspace share
+ *   no memory with each other or with a gradient.
  */
 size_t vp_grad_workspace_bytes(int32_t n);
 vp_status vp_grad_norm(const void* const* grads, const int64_t* counts, const int32_t* dts, int32_t n, float* norm,
@@ -363,7 +364,7 @@ vp_status vp_grad_clip(const void* const* grads, const int64_t* counts, const in
 
 /*
  * The second half of vp_grad_clip alone, with a norm that is known already (such as one summed over several devices):
- * norm [1] is in.
+ * norm [1] is in; it shares no memory with an output.
  */
 vp_status vp_grad_scale(const void* const* grads, const int64_t* counts, const int32_t* dts, int32_t n, void* const* outs,
                         float max_norm, const float* norm, void* workspace, size_t workspace_bytes, void* stream);

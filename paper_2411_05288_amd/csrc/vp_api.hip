@@ -132,6 +132,11 @@ GemmBf16Params logits_product(const void* H, const int64_t* labels, int64_t N, i
 
 bool finite(float v) { return v - v == 0.f; }
 
+// Whether two ranges of memory share a byte.
+bool overlap(const void* p, size_t bytes, const void* q, size_t more) {
+    return (uintptr_t)p < (uintptr_t)q + more && (uintptr_t)q < (uintptr_t)p + bytes;
+}
+
 // Arguments of the norms around a block that both directions have.
 bool norm_args_ok(const void* y, const void* gate, int64_t gate_rows, const void* w_post, const void* b_post, int64_t N,
                   uint32_t flags, float scale) {
@@ -992,7 +997,16 @@ static vp_status grad_call(const void* const* grads, const int64_t* counts, cons
         total += counts[k];
     }
     if (!aligned16(workspace)) return VP_ERR_INVALID_ARG;
-    if (!workspace || workspace_bytes < grad_workspace(n)) return VP_ERR_WORKSPACE;
+    const size_t need = grad_workspace(n);
+    if (!workspace || workspace_bytes < need) return VP_ERR_WORKSPACE;
+    // (a norm that is known is an input)
+    if (overlap(workspace, need, norm, 4)) return VP_ERR_INVALID_ARG;
+    for (int32_t k = 0; k < n; ++k) {
+        const size_t bytes = (size_t)counts[k] * (dts[k] == VP_BF16 ? 2 : 4);
+        if (!bytes) continue;
+        if (overlap(workspace, need, grads[k], bytes) || (!(known && outs) && overlap(norm, 4, grads[k], bytes))) return VP_ERR_INVALID_ARG;
+        if (outs && (overlap(workspace, need, outs[k], bytes) || overlap(norm, 4, outs[k], bytes))) return VP_ERR_INVALID_ARG;
+    }
     return dev(launch_grad(grads, counts, dts, n, outs, max_norm, known, norm, workspace, (hipStream_t)stream));
 }
 

@@ -139,3 +139,56 @@ def test_clip_gradients_of_a_changed_tensor(library, monkeypatch, change):
     counts = [list(args[1]) for _, args in library.calls]
     assert counts == [[128, 100], [128, other.numel()]]
     assert library.calls[1][1][0][1] == other.data_ptr()
+
+
+@pytest.fixture(scope="module")
+def real():
+    import paper_2411_05288_amd as vp
+    return vp.load_library()
+
+
+def refused(real, name, grads, outs, norm, ws, n_bytes=1 << 14):
+    """Whether the library refuses a call with these (address, fp32 elements) lists; the addresses are none, so one that it does
+    not refuse ends with a device error where there is no GPU."""
+    import ctypes
+    n = len(grads)
+    a = [(ctypes.c_void_p * n)(*[p for p, _ in grads]), (ctypes.c_int64 * n)(*[c for _, c in grads]), (ctypes.c_int32 * n)(), n]
+    if name != "vp_grad_norm":
+        a += [None if outs is None else (ctypes.c_void_p * n)(*outs), 1.0]
+    return getattr(real, name)(*a, norm, ws, n_bytes, None) == 1      # VP_ERR_INVALID_ARG
+
+
+NAMES = ("vp_grad_norm", "vp_grad_clip", "vp_grad_scale")
+A, G, O, W = 0x100000, 0x200000, 0x300000, 0x400000      # addresses apart from one another
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the addresses are none")
+@pytest.mark.parametrize("name", NAMES)
+def test_the_norm_and_the_workspace_are_apart_from_the_gradients(real, name):
+    """They are written while gradients are read (the norm is read by vp_grad_scale while they are written)."""
+    for at in (G, G + 4, G + 396):
+        assert refused(real, name, [(A, 10), (G, 100)], None, at, W)
+    size = real.vp_grad_workspace_bytes(2)
+    for at in (G, G + 384, G - size + 16, G - size + 1024):
+        assert refused(real, name, [(A, 10), (G, 100)], None, O, at)
+    for at in (W, W + size - 4):
+        assert refused(real, name, [(A, 10), (G, 100)], None, at, W)
+    assert refused(real, name, [(A, 0), (G, 1)], None, G, W)
+    if name != "vp_grad_norm":
+        assert refused(real, name, [(A, 10), (G, 100)], [A, O], O + 396, W)
+        assert refused(real, name, [(A, 10), (G, 100)], [A, O], A, W)
+        for at in (O, O + 384, O - size + 16):
+            assert refused(real, name, [(A, 10), (G, 100)], [A, O], A + 64, at)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the addresses are none")
+@pytest.mark.parametrize("name", NAMES)
+def test_a_norm_and_a_workspace_beside_the_gradients_are_taken(real, name):
+    size = real.vp_grad_workspace_bytes(2)
+    for norm, ws in ((G - 4, W), (G + 400, W), (W - 4, W), (W + size, W), (A, G + 400), (O, G - size), (G, W)):
+        assert not refused(real, name, [(O + 64, 10), (G, 0 if norm == G else 100)], None, norm, ws, n_bytes=size)
+    # what lies behind the bytes that the call needs is not its workspace
+    assert not refused(real, name, [(O, 10), (W + size, 100)], None, A, W)
+    if name == "vp_grad_scale":      # two inputs
+        assert not refused(real, name, [(A, 10), (G, 100)], [O, O + 4096], G, W)
+    assert not refused(real, name, [(A, 10), (G, 100)], [A, G], O, W)
