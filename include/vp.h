@@ -306,7 +306,8 @@ vp_status vp_embed_bwd_group(const void* grad_out, const int64_t* ids, int32_t p
  *   w_post, b_post, w, b [h] : in, type dt, or NULL (1 and 0).
  *   r [N,h] : out, type dt, or NULL (not kept).  H [N,h] : out, type dt.
  *   stats [4,N] : out, fp32, or NULL: m1, rho1 (0 and 1 without VP_NORM_POST), m2, rho2, which the backward call reads.
- * r may be x and H may be y (in place); apart from that no output shares memory with an input or another output.
+ * r may be x and H may be y, or x where y is NULL (in place); apart from that no output shares memory with an input or another
+ * output.
  * Squares are summed in fp32: rows whose sum of squares exceeds 3.4e38 give rho = 0.
  * eps > 0.  Sizes as above, and h <= 2^20, N h < 2^31.
  */

@@ -1,5 +1,6 @@
 // extern "C" entry points of libvp: argument validation, workspace carving and the order of
 // kernel launches for each pass.  No allocation, no synchronisation, no state.
+#include <initializer_list>
 #include <mutex>
 
 #include "vp_internal.h"
@@ -145,6 +146,28 @@ bool norm_args_ok(const void* y, const void* gate, int64_t gate_rows, const void
     if (!y && (gate || (flags & VP_NORM_POST))) return false;
     return (flags & VP_NORM_POST) || (!w_post && !b_post);
 }
+// Buffers of a call (absent ones are NULL); an output may lie exactly where input number `place` does (-1: none).
+struct Input {
+    Input(const void* p, size_t bytes) : p(p), bytes(p ? bytes : 0) {}
+    const void* p;
+    size_t bytes;
+};
+struct Output : Input {
+    Output(const void* p, size_t bytes, int place = -1) : Input(p, bytes), place(place) {}
+    int place;
+};
+bool outputs_apart(std::initializer_list<Input> ins, std::initializer_list<Output> outs) {
+    for (const Output& o : outs) {
+        for (const Input& i : ins) {
+            const bool in_place = &i - ins.begin() == o.place && o.p == i.p;
+            if (!in_place && overlap(o.p, o.bytes, i.p, i.bytes)) return false;
+        }
+        for (const Output* q = outs.begin(); q != &o; ++q)
+            if (overlap(o.p, o.bytes, q->p, q->bytes)) return false;
+    }
+    return true;
+}
+size_t elem_bytes(vp_dtype dt) { return dt == VP_F32 ? 4 : 2; }
 bool norm_sizes_supported(int64_t N, int64_t h) { return N < MAX_ELEMS && h <= MAX_ROW && N * h < MAX_ELEMS; }
 
 // Elements of all gradients together.
@@ -945,6 +968,10 @@ vp_status vp_block_norm_fwd(const void* x, const void* y, const void* gate, int6
     for (const void* q : {x, y, gate, w_post, b_post, w, b, (const void*)r, (const void*)H, (const void*)stats})
         if (!aligned16(q)) return VP_ERR_INVALID_ARG;
     if (!norm_sizes_supported(N, h)) return VP_ERR_UNSUPPORTED;
+    const size_t row = h * elem_bytes(dt), all = N * row;
+    if (!outputs_apart({{x, all}, {y, all}, {gate, gate_rows * row}, {w_post, row}, {b_post, row}, {w, row}, {b, row}},
+                       {{r, all, 0}, {H, all, y ? 1 : 0}, {stats, (size_t)N * 16}}))
+        return VP_ERR_INVALID_ARG;
     BlockNorm p{x, y, gate, w_post, b_post, w, b, r, H, stats, (int)N, (int)h, gate_rows, (flags & VP_NORM_POST) != 0,
                 (flags & VP_NORM_CENTER) != 0, scale, eps};
     return dev(launch_block_norm_fwd(p, dt, (hipStream_t)stream));
@@ -974,6 +1001,12 @@ vp_status vp_block_norm_bwd(const void* dH, vp_dtype dH_dt, const void* dr, cons
     if (!norm_sizes_supported(N, h)) return VP_ERR_UNSUPPORTED;
     const size_t need = vp_block_norm_bwd_workspace_bytes(N, h, gate_rows, flags);
     if (!workspace || workspace_bytes < need) return VP_ERR_WORKSPACE;
+    const size_t row = h * elem_bytes(dt), all = N * row, grads = (size_t)N * h * elem_bytes(grad_dt), sums = h * sizeof(float);
+    if (!outputs_apart({{dH, (size_t)N * h * elem_bytes(dH_dt)}, {dr, grads}, {r, all}, {y, all}, {gate, gate_rows * row}, {w_post, row},
+                        {b_post, row}, {w, row}, {stats, (size_t)N * 16}},
+                       {{dx, grads, 1}, {dy, grads}, {dgate, gate_rows * sums}, {dw_post, sums}, {db_post, sums}, {dw, sums}, {db, sums},
+                        {workspace, need}}))
+        return VP_ERR_INVALID_ARG;
     BlockNormGrad p{dH, dr, r, y, gate, w_post, b_post, w, stats, dx, dy, dgate, dw_post, db_post, dw, db, (int)N, (int)h,
                     gate_rows, (flags & VP_NORM_POST) != 0, (flags & VP_NORM_CENTER) != 0, scale};
     return dev(launch_block_norm_bwd(p, dt, dH_dt, grad_dt, workspace, (hipStream_t)stream));

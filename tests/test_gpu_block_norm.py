@@ -384,3 +384,38 @@ def test_every_backward_kernel(N, h, post, gate, bias, dtype, dH_type, grad):
         ref.check(name, out[name][0], *expected[name])
         assert out[name][1](), name
     assert ws_ok()
+
+
+@pytest.mark.parametrize("N,h,dtype", [(9, 1000, F32), (700, 77, BF16), (700, 205, BF16), (300, 4099, BF16), (40, 9001, F32), (20, 18437, BF16),
+                                       (2, 40000, F32), (50, 5, BF16)])
+@pytest.mark.parametrize("center", [False, True])
+def test_norm_alone_in_place(N, h, dtype, center):
+    import paper_2411_05288_amd as vp
+    s = inputs(N, h, dtype, False, 0, True, 3)
+    H, stats = torch.empty_like(s["x"]), torch.empty(4, N, device="cuda")
+    vp.vp_block_norm_fwd(s["x"], None, H, stats=stats, w=s["w"], b=s["b"], center=center)
+    x = s["x"].clone()
+    vp.vp_block_norm_fwd(x, None, x, w=s["w"], b=s["b"], center=center)
+    assert torch.equal(x, H)
+
+
+def test_outputs_that_share_memory_are_refused():
+    import paper_2411_05288_amd as vp
+    N, h = 6, 64
+    s = inputs(N, h, BF16, True, 3, True, 1)
+    opts = dict(gate=s["gate"], w_post=s["w_post"], b_post=s["b_post"], post=True)
+    kept = {k: v.clone() for k, v in s.items()}
+    H, r, stats = torch.empty_like(s["x"]), torch.empty_like(s["x"]), torch.ones(4, N, device="cuda")
+    for wrong in (dict(H=s["x"]), dict(r=s["y"]), dict(r=H), dict(H=s["y"], r=s["y"]), dict(x=s["y"], H=s["y"])):
+        with pytest.raises(vp.VPError, match="vp_block_norm_fwd failed: VP_ERR_INVALID_ARG"):
+            vp.vp_block_norm_fwd(**{**dict(x=s["x"], y=s["y"], H=H, r=r, stats=stats, w=s["w"], b=s["b"]), **opts, **wrong})
+    whole = torch.ones(1 << 18, device="cuda")
+    dH, dr, ws = whole[:N * h].view(N, h), torch.ones(N, h, device="cuda"), torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    dx, dy, dw = torch.empty_like(dH), torch.empty_like(dH), torch.empty(h, device="cuda")
+    for wrong in (dict(dx=dH), dict(dy=dr), dict(dy=dx), dict(dw=dx[0]), dict(dw=dH[1]), dict(dw_post=dw), dict(workspace=whole.view(torch.uint8)),
+                  dict(dgate=dr[:3]), dict(dgate=dx[2:5])):
+        with pytest.raises(vp.VPError, match="vp_block_norm_bwd failed: VP_ERR_INVALID_ARG"):
+            vp.vp_block_norm_bwd(**{**dict(dH=dH, r=s["x"], y=s["y"], stats=stats, dx=dx, dy=dy, dr=dr, w=s["w"], dw=dw, workspace=ws), **opts, **wrong})
+    torch.cuda.synchronize()
+    assert all(torch.equal(v, kept[k]) for k, v in s.items())
+    assert all(bool((t == 1).all()) for t in (dH, dr, stats))

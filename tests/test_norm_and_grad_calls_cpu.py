@@ -192,3 +192,60 @@ def test_a_norm_and_a_workspace_beside_the_gradients_are_taken(real, name):
     if name == "vp_grad_scale":      # two inputs
         assert not refused(real, name, [(A, 10), (G, 100)], [O, O + 4096], G, W)
     assert not refused(real, name, [(A, 10), (G, 100)], [A, G], O, W)
+
+
+# Buffers of a call of N=8 h=16 bf16, apart from one another; gradients of activations are fp32.
+N, H_ = 8, 16
+BYTES = dict(x=256, y=256, r=256, H=256, stats=128, gate=64, w=32, b=32, w_post=32, b_post=32, dH=256, dr=512, dx=512, dy=512, dgate=128,
+             dw=64, db=64, dw_post=64, db_post=64)
+AT = {k: 0x100000 * (i + 1) for i, k in enumerate(BYTES)}
+FWD_IN, FWD_OUT = ("x", "y", "gate", "w_post", "b_post", "w", "b"), ("r", "H", "stats")
+BWD_IN = ("dH", "dr", "r", "y", "gate", "w_post", "b_post", "w", "stats")
+BWD_OUT = ("dx", "dy", "dgate", "dw_post", "db_post", "dw", "db", "ws")
+W_BYTES = 1 << 20
+
+
+def norm_call(real, forward, **at):
+    """Status of a call with everything, with the buffers of `at` elsewhere (None: not given)."""
+    p = {**AT, "ws": W << 8, **at}
+    rows = 2 if p["gate"] else 0
+    if forward:
+        return real.vp_block_norm_fwd(p["x"], p["y"], p["gate"], rows, p["w_post"], p["b_post"], p["w"], p["b"], N, H_, 1, 24 if p["y"] else 16, 1.0,
+                                      1e-5, p["r"], p["H"], p["stats"], None)
+    return real.vp_block_norm_bwd(p["dH"], 1, p["dr"], p["r"], p["y"], p["gate"], rows, p["w_post"], p["b_post"], p["w"], p["stats"], N, H_, 1,
+                                  24 if p["y"] else 16, 1.0, 0, p["dx"], p["dy"], p["dgate"], p["dw_post"], p["db_post"], p["dw"], p["db"],
+                                  p["ws"], W_BYTES, None)
+
+
+def beside(other, name, size):
+    """Places of a buffer that share memory with another one: its first and last 16 bytes, and all of it."""
+    return (AT[other], AT[other] + BYTES[other] - 16, AT[other] - size(name) + 16)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the addresses are none")
+@pytest.mark.parametrize("forward", [True, False])
+def test_outputs_of_the_norms_are_apart(real, forward):
+    ins, outs = (FWD_IN, FWD_OUT) if forward else (BWD_IN, BWD_OUT)
+    need = real.vp_block_norm_bwd_workspace_bytes(N, H_, 2, 24)
+
+    def size(k):
+        return BYTES.get(k, need)
+    in_place = {("r", "x"), ("H", "y")} if forward else {("dx", "dr")}
+    assert norm_call(real, forward) != 1
+    for out in outs:
+        for other in ins + tuple(o for o in outs if o != out and o != "ws"):
+            for at in beside(other, out, size):
+                ok = (out, other) in in_place and at == AT[other]
+                assert (norm_call(real, forward, **{out: at}) == 1) != ok, (out, other, hex(at))
+    if forward:
+        assert norm_call(real, True, r=AT["x"], H=AT["y"]) != 1
+        assert norm_call(real, True, r=AT["x"], y=AT["x"]) == 1 and norm_call(real, True, x=AT["y"], H=AT["y"]) == 1
+        assert norm_call(real, True, y=AT["x"]) != 1      # two inputs
+        alone = dict(y=None, gate=None, r=None, w_post=None, b_post=None)
+        assert norm_call(real, True, H=AT["x"], **{**alone, "y": None}) != 1
+        assert norm_call(real, True, H=AT["x"] + 16, **alone) == 1
+        assert norm_call(real, True, r=None, H=AT["r"]) != 1 and norm_call(real, True, stats=None, H=AT["stats"]) != 1
+    else:
+        assert norm_call(real, False, dr=None, dx=AT["dr"]) != 1 and norm_call(real, False, dr=AT["dH"]) != 1
+        assert norm_call(real, False, dx=AT["dr"], dH=AT["dr"]) == 1
+        assert norm_call(real, False, ws=AT["dx"] - need) != 1 and norm_call(real, False, ws=AT["dx"] + BYTES["dx"]) != 1
