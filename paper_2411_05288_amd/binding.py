@@ -552,8 +552,8 @@ def _norm_flags(post: bool, center: bool) -> int:
 def _gate_rows(gate) -> int:
     if gate is None:
         return 0
-    if gate.dim() != 2:
-        raise VPError("gate must be [rows, h]")
+    if gate.dim() != 2 or gate.shape[0] == 0:
+        raise VPError("gate must be [rows, h], with a row at least")
     return gate.shape[0]
 
 

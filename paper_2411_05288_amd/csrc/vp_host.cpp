@@ -190,10 +190,11 @@ struct Call {
         ok = true;
         return t.data_ptr();
     }
-    // N and h of a matrix; a gate's rows (0 for None)
+    // N and h of a matrix; a gate's rows (0 for None; a gate without rows has no address and would be taken for none)
     int64_t size(PyObject* o, int64_t d) {
         if (o == Py_None) return 0;
-        if (!THPVariable_CheckExact(o) || !THPVariable_Unpack(o).defined() || THPVariable_Unpack(o).dim() != 2) {
+        if (!THPVariable_CheckExact(o) || !THPVariable_Unpack(o).defined() || THPVariable_Unpack(o).dim() != 2 ||
+            THPVariable_Unpack(o).size(d) == 0) {
             ok = false;
             return 0;
         }

@@ -419,3 +419,24 @@ def test_outputs_that_share_memory_are_refused():
     torch.cuda.synchronize()
     assert all(torch.equal(v, kept[k]) for k, v in s.items())
     assert all(bool((t == 1).all()) for t in (dH, dr, stats))
+
+
+def test_a_gate_without_rows_is_refused(monkeypatch):
+    """The same by the native checks and by those in Python."""
+    import paper_2411_05288_amd as vp
+    import paper_2411_05288_amd.binding as B
+    N, h = 4, 64
+    x, y, gate = torch.ones(N, h, device="cuda"), torch.ones(N, h, device="cuda"), torch.empty(0, h, device="cuda")
+    H, stats, dx, dy = torch.full_like(x, 7.0), torch.ones(4, N, device="cuda"), torch.full_like(x, 7.0), torch.full_like(x, 7.0)
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    B.load_library()
+    for host in (B._HOST, None):
+        monkeypatch.setattr(B, "_HOST", host)
+        with pytest.raises(vp.VPError, match="gate must be"):
+            vp.vp_block_norm_fwd(x, y, H, gate=gate)
+        with pytest.raises(vp.VPError, match="gate must be"):
+            vp.vp_block_norm_bwd(x, x, y, stats, dx=dx, dy=dy, gate=gate, workspace=ws)
+        with pytest.raises(vp.VPError, match="gate must be"):
+            vp.BlockNormPlan(x, y, gate=gate).forward()
+    torch.cuda.synchronize()
+    assert all(bool((t == 7).all()) for t in (H, dx, dy))

@@ -249,3 +249,16 @@ def test_outputs_of_the_norms_are_apart(real, forward):
         assert norm_call(real, False, dr=None, dx=AT["dr"]) != 1 and norm_call(real, False, dr=AT["dH"]) != 1
         assert norm_call(real, False, dx=AT["dr"], dH=AT["dr"]) == 1
         assert norm_call(real, False, ws=AT["dx"] - need) != 1 and norm_call(real, False, ws=AT["dx"] + BYTES["dx"]) != 1
+
+
+def test_a_gate_without_rows_is_refused(library, monkeypatch):
+    """It has no address, and would be taken for no gate at all."""
+    import paper_2411_05288_amd as vp
+    import paper_2411_05288_amd.binding as B
+    monkeypatch.setattr(B, "_HOST", None)
+    x, y, H, stats, gate = torch.zeros(4, 8), torch.zeros(4, 8), torch.zeros(4, 8), torch.zeros(4, 4), torch.zeros(0, 8)
+    with pytest.raises(vp.VPError, match="gate must be"):
+        vp.vp_block_norm_fwd(x, y, H, gate=gate)
+    with pytest.raises(vp.VPError, match="gate must be"):
+        vp.vp_block_norm_bwd(x, x, y, stats, dx=H, dy=torch.zeros(4, 8), gate=gate, workspace=torch.zeros(1 << 16, dtype=torch.uint8))
+    assert library.calls == []
