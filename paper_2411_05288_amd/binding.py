@@ -76,8 +76,7 @@ def load_library() -> ctypes.CDLL:
     path = lib_path()
     if not os.path.exists(path):
         raise VPError("libvp.so not found at %s: build it with `python -m paper_2411_05288_amd.build`" % path)
-    if _HOST is None:
-        _HOST = _load_host(host_path())
+    host = _load_host(host_path()) if _HOST is None else _HOST
     lib = ctypes.CDLL(path)
     c = ctypes
     vp, i64, i32, u32, sz, fl = c.c_void_p, c.c_int64, c.c_int32, c.c_uint32, c.c_size_t, c.c_float
@@ -162,7 +161,7 @@ def load_library() -> ctypes.CDLL:
     lib.vp_profile_read.argtypes = [c.POINTER(c.c_double), c.POINTER(c.c_int64), c.c_int]
     for name in ("vp_block_norm_fwd", "vp_block_norm_bwd"):
         _ADDRESS[name] = c.cast(getattr(lib, name), vp).value
-    _LIB = lib
+    _LIB, _HOST = lib, host      # (only now: the native checks call the library's functions)
     return lib
 
 

@@ -262,3 +262,22 @@ def test_a_gate_without_rows_is_refused(library, monkeypatch):
     with pytest.raises(vp.VPError, match="gate must be"):
         vp.vp_block_norm_bwd(x, x, y, stats, dx=H, dy=torch.zeros(4, 8), gate=gate, workspace=torch.zeros(1 << 16, dtype=torch.uint8))
     assert library.calls == []
+
+
+def test_a_library_that_cannot_be_loaded_says_so_every_time(monkeypatch, tmp_path):
+    """After a load that failed, a call tries again: it does not look for the functions of a library that is not there."""
+    import paper_2411_05288_amd as vp
+    import paper_2411_05288_amd.binding as B
+    broken = tmp_path / "libvp.so"
+    broken.write_text("no library")
+    for name, value in (("_LIB", None), ("_HOST", None), ("_ADDRESS", {}), ("lib_path", lambda: str(broken)), ("_on_current_device", lambda ts: None)):
+        monkeypatch.setattr(B, name, value)
+    x, y, stats, ws = torch.zeros(4, 8), torch.zeros(4, 8), torch.zeros(4, 4), torch.zeros(1 << 16, dtype=torch.uint8)
+    for _ in range(2):
+        with pytest.raises(OSError):
+            B.load_library()
+        with pytest.raises(OSError):
+            vp.vp_block_norm_fwd(x, None, y)
+        monkeypatch.setattr(B, "_ptr", lambda t, *_: None if t is None else t.data_ptr())
+        with pytest.raises(OSError):
+            vp.vp_block_norm_bwd(x, x, None, stats, dx=y, workspace=ws)
