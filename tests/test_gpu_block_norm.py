@@ -440,3 +440,23 @@ def test_a_gate_without_rows_is_refused(monkeypatch):
             vp.BlockNormPlan(x, y, gate=gate).forward()
     torch.cuda.synchronize()
     assert all(bool((t == 7).all()) for t in (H, dx, dy))
+
+
+@pytest.mark.parametrize("N,large", [(N, at) for N in (96, 128, 256) for at in (0, 1, 37)])
+def test_sums_over_few_tokens_lose_little(N, large):
+    """Up to 256 tokens of 256 columns: at most 7 additions in a row for the tokens of a slice (256 / 32 of them), then 5 levels of a
+    tree over 32 slices, so 12 roundings relative to the sum of absolute values.  Slices of N / 32 beside a value of which that is
+    half a step are lost one by one where they are added to it in a row."""
+    import paper_2411_05288_amd as vp
+    h = 256
+    dH = torch.ones(N, h, device="cuda")
+    value = 2.0 ** (26 if N <= 128 else 27)
+    dH[large] = value
+    x, stats = torch.full((N, h), 0.5, device="cuda"), torch.ones(4, N, device="cuda")
+    stats[2] = 0.0      # rh = x
+    ws = torch.full((vp.vp_block_norm_bwd_workspace_bytes(N, h),), 0xFF, dtype=torch.uint8, device="cuda")
+    dw, db, dx = torch.empty(h, device="cuda"), torch.empty(h, device="cuda"), torch.empty_like(x)
+    vp.vp_block_norm_bwd(dH, x, None, stats, dx=dx, dw=dw, db=db, workspace=ws)
+    for got, exact in ((db, value + N - 1), (dw, (value + N - 1) / 2)):
+        off = float((got.double() - exact).abs().max())
+        assert off <= 12 * ref.U * exact, off
