@@ -394,3 +394,59 @@ def test_plan_notices_gradients_that_changed_where_they_are():
     total = plan.clip_gradients(1.0, [other])
     assert plan.clip_plan.arguments.dts[-1] == vp.VP_BF16 and abs(float(total) - 20) <= 1e-4      # 10 * 2 and what is left of dW
     assert bool((whole[100:] == 3).all())
+
+
+def long_lists():
+    """(name, numbers of elements) around the 160 tensors that the kernel arguments hold, full batches of a table, and the 2048 of
+    whose first chunks a workgroup holds every one (above that every second, every third)."""
+    for n in (159, 160, 161, 319, 320, 321, 480, 481):
+        yield "%d" % n, [k * 13 % 61 for k in range(n)]
+    for n in (2047, 2048, 2049, 4096, 4097, 5000):
+        yield "%d" % n, [k * 29 % 97 for k in range(n)]
+    # tensors without elements where every second one is looked up, at the ends of what lies between, and at both ends of the list
+    yield "empty ones that are looked up", [0 if k % 2 == 0 else k % 50 + 1 for k in range(4000)]
+    yield "empty ones between", [0 if k % 2 else k % 50 + 1 for k in range(4000)]
+    yield "empty runs", [0 if k // 5 % 3 else k % 50 + 1 for k in range(5001)]
+    yield "empty ends", [0] * 1000 + [7] * 2000 + [0] * 1000
+    yield "one of many", [0] * 3000 + [33] + [0] * 1999
+    yield "none of many", [0] * 2500
+    # tensors of several chunks among small ones
+    yield "large ones between", [30011 if k % 500 == 17 else k % 9 for k in range(4500)]
+
+
+@pytest.mark.parametrize("name,counts", list(long_lists()), ids=[n for n, _ in long_lists()])
+@pytest.mark.parametrize("mixed", [False, True])
+def test_long_lists(name, counts, mixed):
+    """Views of one buffer per type, in place and into the views of another; every element of the buffers is looked at, those between
+    the tensors too."""
+    import paper_2411_05288_amd as vp
+    types = [BF16 if mixed and k % 3 == 1 else F32 for k in range(len(counts))]
+    gap = 3      # elements between two tensors
+    size = {t: sum(n + gap for n, u in zip(counts, types) if u == t) + gap for t in (F32, BF16)}
+    g = torch.Generator(device="cuda").manual_seed(len(counts))
+    whole = {t: torch.randn(n, generator=g, device="cuda").to(t) for t, n in size.items()}
+    inside = {t: torch.zeros(n, dtype=torch.bool) for t, n in size.items()}
+    at, spans = dict.fromkeys(size, gap), []
+    for n, t in zip(counts, types):
+        spans.append((t, at[t], n))
+        inside[t][at[t]:at[t] + n] = True
+        at[t] += n + gap
+    inside = {t: m.cuda() for t, m in inside.items()}
+
+    def views(buffers):
+        return [buffers[t][a:a + n] for t, a, n in spans]
+    expected = math.sqrt(math.fsum(float(whole[t].double()[inside[t]].square().sum()) for t in whole))
+    most = expected / 3 if expected else 1.0
+    norm, ws = torch.full((1,), 7.0, device="cuda"), torch.full((vp.vp_grad_workspace_bytes(len(counts)),), 0xFF, dtype=torch.uint8, device="cuda")
+    vp.vp_grad_norm(views(whole), norm, ws)
+    assert abs(float(norm) - expected) <= expected * (2.0 ** -24 + 1e-12)
+    outs, here, known = ({t: b.clone() for t, b in whole.items()} for _ in range(3))
+    for buffers, call in ((outs, lambda b: vp.vp_grad_clip(views(whole), most, norm, ws, outs=views(b))),
+                          (here, lambda b: vp.vp_grad_clip(views(b), most, norm, ws)),
+                          (known, lambda b: vp.vp_grad_scale(views(b), most, norm, ws))):
+        ws.fill_(0xFF)
+        call(buffers)
+        for t, b in buffers.items():
+            assert torch.equal(b[~inside[t]], whole[t][~inside[t]])
+            if expected:
+                check_clipped(b[inside[t]], whole[t][inside[t]], 1 / 3)
