@@ -163,9 +163,13 @@ struct Kinds {
     static constexpr int SLOTS = LDS1 > LDS0 ? LDS1 - LDS0 : (C == 1 ? 1 : 0);
 };
 
-// Rows of 8 to 8192 C columns in one pass (N=512 h=32768 bf16: 112 us, with a launch for each step 290): a row's values stay on
-// the chip between the sums over it and dx and dy, and a thread's columns are the same in every row of its range, so the sums
-// over tokens stay there too.
+// Rows of 8 to 8192 C columns in one pass (N=512 h=32768 bf16: 117 us, with a launch for each step 290).  C = 1: a row's values
+// stay in registers between the sums over it and dx and dy, and a thread's columns are the same in every row of its range, so the
+// sums over tokens stay on the chip too.  C > 1: the inputs are read again for every step, from the caches (below), and some of the
+// sums over tokens go through the L2 (Kinds, above).
+//
+// Of 128 registers a thread, 68 of the 200 instances spill: with C = 4 all (bf16 2 to 82 registers, fp32 28 to 107), and with a post norm
+// and a gate together most others (1 to 26; bf16 with whole wavefronts and C = 1 at most 2).
 //
 // A workgroup fills a CU (up to 1024 threads of up to 128 registers), with as many rows at a time as it holds: fewer partial sums
 // to write and add up than with a workgroup per row (N=4096 h=4096: 256 rows of them in place of 512).
@@ -239,7 +243,7 @@ __global__ __launch_bounds__(1024) void block_norm_bwd_kernel(BlockNormGrad p, C
     };
     // What is read of a row.  C = 1: once, and kept in registers from the first sums to the last.  C > 1: again in every step, from
     // the caches (two vectors of everything at once do not fit: N=2048 h=16384, kept, 124 us for bf16 RMS norms, 215 for fp32 ones
-    // and 270 with everything; read again, 127, 196 and 257).
+    // and 270 with everything; read again, 127, 196 and 257, which a third kind of sums in registers made 227).
     struct Values {
         Raw8<TD> dH;
         Raw8<TG> dr;

@@ -1,7 +1,7 @@
 // The norms before and after a block of the model with its gate and residual scale, forward and backward (vp.h has the
 // formulas).  Bound by HBM: the forward call reads x and y and writes r and H, the backward call reads dH, dr, r and y and
 // writes dx and dy, each once if a row stays on the chip between the sums over it and their use.  N=4096 h=4096 bf16, RMS norms
-// on both sides: forward 26.5 us (5.1 TB/s), backward with fp32 dH 47.1 us (5.2 TB/s) and 4.7 us for the last sums over tokens; a
+// on both sides: forward 26.5 us (5.1 TB/s), backward with fp32 dH 47.5 us (5.1 TB/s) and 4.8 us for the last sums over tokens; a
 // single token 3.4 us.
 #include "vp_block_norm.h"
 

@@ -1,7 +1,7 @@
 // The norm of all gradients of a step together, and clipping by it.
 //
 // Bound by HBM: the norm reads every gradient once (8 x 4000 x 4096 fp32: 77 us, 6.8 TB/s), clipping reads it again and writes it
-// (8 x 16032 x 4096: 310 us, then 768 us, 5.5 TB/s); short lists by the two launches.  A call has n tensors of any size
+// (8 x 16032 x 4096: 301 us, then 765 us, 5.5 TB/s); short lists by the two launches.  A call has n tensors of any size
 // and either type; they are cut into chunks of 32 KB, the chunks are numbered through over all tensors, and the workgroups of
 // one launch share them, so a thousand small tensors and eight large ones fill the chip alike.  The tensors travel in the
 // kernel arguments, or, where there are more than fit, in a table in the workspace that a small kernel writes from its
