@@ -332,11 +332,12 @@ class OutputLayerPlan:
         grads = self.dW + (self.norm.parameter_gradients() if self.norm is not None else []) + list(others)
         if self.clip_plan is None or not self.clip_plan.covers(grads):
             # the norm and the workspaces stay where they are as long as this plan lives: a captured call has their addresses
-            if self.clip_norm is None:
-                self.clip_norm = torch.empty((1,), dtype=torch.float32, device=self.dH.device)
             need = B.vp_grad_workspace_bytes(len(grads))
-            if not self.clip_workspaces or self.clip_workspaces[-1].numel() < need:
-                self.clip_workspaces.append(torch.empty((need,), dtype=torch.uint8, device=self.dH.device))
+            with self._on(stream):      # (the memory of a stream: the current one's may be in use by work before this call)
+                if self.clip_norm is None:
+                    self.clip_norm = torch.empty((1,), dtype=torch.float32, device=self.dH.device)
+                if not self.clip_workspaces or self.clip_workspaces[-1].numel() < need:
+                    self.clip_workspaces.append(torch.empty((need,), dtype=torch.uint8, device=self.dH.device))
             self.clip_plan = GradientClipPlan(grads, norm=self.clip_norm, workspace=self.clip_workspaces[-1])
         self.clip_plan.clip(max_norm, stream)
         return self.clip_norm

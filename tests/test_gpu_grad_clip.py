@@ -450,3 +450,25 @@ def test_long_lists(name, counts, mixed):
             assert torch.equal(b[~inside[t]], whole[t][~inside[t]])
             if expected:
                 check_clipped(b[inside[t]], whole[t][inside[t]], 1 / 3)
+
+
+@pytest.mark.parametrize("as_number", [False, True])
+def test_clipping_on_another_stream_takes_its_memory_there(as_number):
+    """What a call on a stream allocates belongs to that stream: memory freed by work that is still running on the current one may
+    not be written from another."""
+    import paper_2411_05288_amd as vp
+    plan = vp.OutputLayerPlan(torch.randn(16, 32, device="cuda"), [torch.randn(64, 32, device="cuda")],
+                              torch.zeros(16, dtype=torch.int64, device="cuda"))
+    plan.step()
+    torch.cuda.synchronize()
+    before = [t.clone() for t in plan.dW]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    total = plan.clip_gradients(1e-3, stream=side.cuda_stream if as_number else side)
+    side.synchronize()
+    expected = exact_norm(before)
+    assert abs(float(total) - expected) <= 2.0 ** -23 * expected
+    check_clipped(plan.dW[0], before[0], 1e-3 / expected)
+    for t in (plan.clip_norm, plan.clip_workspaces[-1]):
+        (segment,) = [s for s in torch.cuda.memory_snapshot() if s["address"] <= t.data_ptr() < s["address"] + s["total_size"]]
+        assert segment["stream"] == side.cuda_stream
