@@ -371,6 +371,72 @@ vp_status vp_grad_scale(const void* const* grads, const int64_t* counts, const i
                         float max_norm, const float* norm, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * The output layer from weights and hidden states in 8-bit integers, for answering and scoring.  vp_quantize_rows makes integers
+ * of the rows of a matrix, of the hidden states (a scale for each token) and of the vocabulary's (a scale for each row of W):
+ *     a_i = max_j |x_ij|,   scales[i] = a_i / 127,   q_ij = 127 x_ij / a_i rounded to the nearest integer, ties to even
+ * The quotient is the exact one, so q does not depend on the order or width of any arithmetic.  A row of zeros has scale 0 and
+ * q = 0; a row that holds an infinity or a NaN has scale NaN and q = 0 (its logits become NaN, other rows' do not).
+ *   x [N,h] : in, type dt.   q [N, vp_i8_row_stride(h)] : out, int8, zero in the columns h and behind.   scales [N] : out, fp32.
+ * vp_i8_row_stride: h rounded up to a multiple of 128 (-1 for h < 1 or h > 130944: sums of products stay below 2^31).
+ */
+int64_t vp_i8_row_stride(int64_t h);
+vp_status vp_quantize_rows(const void* x, int64_t N, int64_t h, vp_dtype dt, int8_t* q, float* scales, void* stream);
+
+/*
+ * vp_output_fwd from integers and their scales, for one shard:
+ *     Y_ij = H_scales[i] * W_scales[j] * sum_k H_ik W_jk          (the sum exact, in 32 bits)
+ * and the statistics of Y as there.  k is the row stride of both matrices, a multiple of 128; columns that stand for nothing
+ * are zero (in one of the two at least).  logits_out (with VP_SAVE_LOGITS) is of type logits_dt.  A temperature is a factor of
+ * H_scales.
+ *   H [N,k], W_shard [Vs,k] : in, int8.  H_scales [N], W_scales [Vs] : in, fp32, finite and not negative (a NaN makes its row or
+ *   column of the logits NaN), at any element.   Everything else as for vp_output_fwd.  No output shares memory with an input or another output.
+ * The workspace has vp_output_i8_workspace_bytes(1, N, &Vs) bytes ((size_t)-1 for invalid arguments).
+ *
+ * vp_output_fwd_i8_group: p shards that live on one device, arguments as for vp_output_fwd_group (W_shards, W_scales and
+ * logits_out HOST arrays of p device pointers), results those of p single calls.
+ */
+size_t vp_output_i8_workspace_bytes(int32_t p, int64_t N, const int64_t* rows);
+vp_status vp_output_fwd_i8(const int8_t* H, const float* H_scales, const int8_t* W_shard, const float* W_scales,
+                           const int64_t* labels, int64_t N, int64_t k, int64_t Vs, int64_t shard_offset, vp_dtype logits_dt,
+                           uint32_t flags, float* local_max, float* local_sumexp, float* local_target, void* logits_out,
+                           void* workspace, size_t workspace_bytes, void* stream);
+vp_status vp_output_fwd_i8_group(const int8_t* H, const float* H_scales, const int8_t* const* W_shards,
+                                 const float* const* W_scales, const int64_t* rows, const int64_t* shard_offsets, int32_t p,
+                                 const int64_t* labels, int64_t N, int64_t k, vp_dtype logits_dt, uint32_t flags,
+                                 float* local_max, float* local_sumexp, float* local_target, void* const* logits_out,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Verification of drafted tokens against the logits of p shards (at most 64) that live on one device, and the draw of the token
+ * behind them (speculative sampling).  Sequence b has the rows starts[b] .. starts[b+1] - 1 of the logits: one for each of its
+ * drafts, drafts[i] the token that row i is asked about, and a last one without (a sequence of one row is plain sampling).
+ * With p_ij = exp(Y_ij - global_max[i]) / global_sumexp[i] and q_ij the same of the draft model's logits and statistics, row by
+ * row (of its last rows nothing is read), or q all on drafts[i] where there is no draft model (draft_logits == NULL):
+ *     draft i is accepted if uniforms[i] * q_i(drafts[i]) < p_i(drafts[i]) and all drafts of the sequence before it were;
+ *     the next token is drawn from w_j = max(p_ij - q_ij, 0) of the first rejected row i, or from w = p of the last row: the
+ *     first token, in the order of the shards, at which the running sum of w exceeds uniforms[last row] * (sum of w).
+ * Where that sum is 0 (p nowhere above q: roundings of the statistics) it is drawn from p.  A row without a single possible
+ * token (all logits -inf, or a NaN or +inf among them) gives the token -1.
+ * Probabilities and sums are held in 64 bits, in a fixed order: results repeat bit for bit.
+ *   logits, draft_logits : HOST arrays of p device pointers to [N, rows[r]], in, type dt, or NULL for draft_logits; they may start
+ *   at any element.  -inf rules a token out.  The shards' ranges of the vocabulary do not overlap.
+ *   global_max, global_sumexp [N] : in, fp32, as vp_combine_stats leaves them.  draft_max, draft_sumexp [N] : in, or NULL.
+ *   drafts [N] : in, int64; a draft that no shard owns is rejected, those of last rows are ignored.
+ *   starts [sequences + 1] : in, int64, ascending, within [0, N] (values outside are taken as the nearest bound; a sequence
+ *   without rows has 0 accepted and writes no tokens).   uniforms [N] : in, fp32, in [0, 1).
+ *   accepted [sequences] : out, int32, accepted drafts.  tokens [N] : out, int64: in a sequence's rows its accepted drafts, the
+ *   next token, and -1 behind it.  Rows of no sequence are left as they were.  No output shares memory with an input or another
+ *   output.
+ * The workspace has vp_verify_workspace_bytes(sequences, V) bytes, V = the sum of rows ((size_t)-1 for invalid arguments).
+ */
+size_t vp_verify_workspace_bytes(int32_t sequences, int64_t V);
+vp_status vp_verify_drafts(const void* const* logits, const int64_t* rows, const int64_t* shard_offsets, int32_t p, vp_dtype dt,
+                           const float* global_max, const float* global_sumexp, const void* const* draft_logits,
+                           const float* draft_max, const float* draft_sumexp, const int64_t* drafts, const int64_t* starts,
+                           const float* uniforms, int64_t N, int32_t sequences, int32_t* accepted, int64_t* tokens,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Measurement aid, not part of the method.  While enabled, every kernel launch made by the
  * entry points above is bracketed by two HIP events on the launch stream, the few launches of one step (an fp32 product and
  * the sum of its K slices, the barrier, the sort of the input layer) by one pair (events are created

@@ -137,6 +137,20 @@ def load_library() -> ctypes.CDLL:
     lib.vp_grad_clip.argtypes = [vp, vp, vp, i32, vp, fl, vp, vp, sz, vp]
     lib.vp_grad_scale.restype = c.c_int
     lib.vp_grad_scale.argtypes = [vp, vp, vp, i32, vp, fl, vp, vp, sz, vp]
+    lib.vp_i8_row_stride.restype = i64
+    lib.vp_i8_row_stride.argtypes = [i64]
+    lib.vp_quantize_rows.restype = c.c_int
+    lib.vp_quantize_rows.argtypes = [vp, i64, i64, c.c_int, vp, vp, vp]
+    lib.vp_output_i8_workspace_bytes.restype = sz
+    lib.vp_output_i8_workspace_bytes.argtypes = [i32, i64, vp]
+    lib.vp_output_fwd_i8.restype = c.c_int
+    lib.vp_output_fwd_i8.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i64, c.c_int, u32, vp, vp, vp, vp, vp, sz, vp]
+    lib.vp_output_fwd_i8_group.restype = c.c_int
+    lib.vp_output_fwd_i8_group.argtypes = [vp, vp, vp, vp, vp, vp, i32, vp, i64, i64, c.c_int, u32, vp, vp, vp, vp, vp, sz, vp]
+    lib.vp_verify_workspace_bytes.restype = sz
+    lib.vp_verify_workspace_bytes.argtypes = [i32, i64]
+    lib.vp_verify_drafts.restype = c.c_int
+    lib.vp_verify_drafts.argtypes = [vp, vp, vp, i32, c.c_int, vp, vp, vp, vp, vp, vp, vp, vp, i64, i32, vp, vp, vp, sz, vp]
     lib.vp_profile_mfma_loop.restype = c.c_int
     lib.vp_profile_mfma_loop.argtypes = [vp, vp, i32, i32, vp]
     lib.vp_profile_mfma_variant.restype = c.c_int
@@ -716,6 +730,125 @@ def vp_grad_clip(grads, max_norm: float, norm, workspace, outs=None, stream=None
 def vp_grad_scale(grads, max_norm: float, norm, workspace, outs=None, stream=None) -> None:
     """vp_grad_clip with a norm that is known already."""
     _grad_call("vp_grad_scale", _gradients(grads, outs), norm, workspace, stream, float(max_norm))
+
+
+def vp_i8_row_stride(h: int) -> int:
+    """Bytes of a row of h elements in 8-bit integers."""
+    n = load_library().vp_i8_row_stride(h)
+    if n < 0:
+        raise VPError("vp_i8_row_stride: invalid arguments")
+    return n
+
+
+def vp_quantize_rows(x, q, scales, stream=None) -> None:
+    """Rows of x [N, h] in 8-bit integers: scales [N] = max |x| / 127, q [N, vp_i8_row_stride(h)] = 127 x / max |x| to the
+    nearest integer, zero behind column h."""
+    if x.dim() != 2:
+        raise VPError("x must be [N, h]")
+    N, h = x.shape
+    _on_current_device((x, q, scales))
+    st = load_library().vp_quantize_rows(
+        _ptr(x, "x"), N, h, _dtype_code(x), _ptr(q, "q", (torch.int8,), (N, vp_i8_row_stride(h))),
+        _ptr(scales, "scales", (torch.float32,), (N,)), _stream(stream))
+    _check(st, "vp_quantize_rows")
+
+
+def vp_output_i8_workspace_bytes(N: int, rows) -> int:
+    n = load_library().vp_output_i8_workspace_bytes(len(rows), N, _i64s(rows))
+    if n == ctypes.c_size_t(-1).value:
+        raise VPError("vp_output_i8_workspace_bytes: invalid arguments")
+    return n
+
+
+def _logits_code(logits_out) -> int:
+    if logits_out is None:
+        return VP_BF16
+    if any(t.dtype != logits_out[0].dtype for t in logits_out):
+        raise VPError("logits_out: tensors of one type")
+    return _dtype_code(logits_out[0])
+
+
+def vp_output_fwd_i8(H, H_scales, W_shard, W_scales, labels, shard_offset: int, local_max, local_sumexp, local_target,
+                     logits_out=None, workspace=None, stream=None) -> None:
+    """vp_output_fwd from 8-bit integers H [N, k] and W_shard [Vs, k] and their scales (vp_quantize_rows); the logits are bf16 or
+    fp32, by the type of logits_out."""
+    if H.dim() != 2 or W_shard.dim() != 2:
+        raise VPError("H must be [N, k] and W_shard [Vs, k]")
+    N, k = H.shape
+    Vs = W_shard.shape[0]
+    i8, f = (torch.int8,), (torch.float32,)
+    logits = None if logits_out is None else [logits_out]
+    dt = _logits_code(logits)
+    _on_current_device((H, H_scales, W_shard, W_scales, labels, local_max, local_sumexp, local_target, logits_out, workspace))
+    wp, wb = _ws(workspace)
+    st = load_library().vp_output_fwd_i8(
+        _ptr(H, "H", i8), _ptr(H_scales, "H_scales", f, (N,)), _ptr(W_shard, "W_shard", i8, (Vs, k)),
+        _ptr(W_scales, "W_scales", f, (Vs,)), _ptr(labels, "labels", (torch.int64,), (N,)), N, k, Vs, shard_offset, dt,
+        VP_SAVE_LOGITS if logits_out is not None else 0, _ptr(local_max, "local_max", f, (N,)),
+        _ptr(local_sumexp, "local_sumexp", f, (N,)), _ptr(local_target, "local_target", f, (N,)),
+        _ptr(logits_out, "logits_out", None, (N, Vs)), wp, wb, _stream(stream))
+    _check(st, "vp_output_fwd_i8")
+
+
+def vp_output_fwd_i8_group(H, H_scales, W_shards, W_scales, labels, shard_offsets, local_max, local_sumexp, local_target,
+                           logits_out=None, workspace=None, stream=None) -> None:
+    """vp_output_fwd_i8 for several shards on this device in one call; the statistics are [p, N]."""
+    if H.dim() != 2 or any(w.dim() != 2 for w in W_shards):
+        raise VPError("H must be [N, k] and W_shards [rows, k]")
+    N, k = H.shape
+    p = len(W_shards)
+    if len(shard_offsets) != p:
+        raise VPError("one offset per shard")
+    rows = [int(w.shape[0]) for w in W_shards]
+    i8, f = (torch.int8,), (torch.float32,)
+    dt = _logits_code(logits_out)
+    _on_current_device((H, H_scales, *W_shards, *W_scales, labels, local_max, local_sumexp, local_target, *(logits_out or ()),
+                        workspace))
+    wp, wb = _ws(workspace)
+    st = load_library().vp_output_fwd_i8_group(
+        _ptr(H, "H", i8), _ptr(H_scales, "H_scales", f, (N,)), _each(W_shards, "W_shards", i8, [(n, k) for n in rows]),
+        _each(W_scales, "W_scales", f, [(n,) for n in rows]), _i64s(rows), _i64s(shard_offsets), p,
+        _ptr(labels, "labels", (torch.int64,), (N,)), N, k, dt, VP_SAVE_LOGITS if logits_out is not None else 0,
+        _ptr(local_max, "local_max", f, (p, N)), _ptr(local_sumexp, "local_sumexp", f, (p, N)),
+        _ptr(local_target, "local_target", f, (p, N)), _each(logits_out, "logits_out", None, [(N, n) for n in rows]),
+        wp, wb, _stream(stream))
+    _check(st, "vp_output_fwd_i8_group")
+
+
+def vp_verify_workspace_bytes(sequences: int, V: int) -> int:
+    n = load_library().vp_verify_workspace_bytes(sequences, V)
+    if n == ctypes.c_size_t(-1).value:
+        raise VPError("vp_verify_workspace_bytes: invalid arguments")
+    return n
+
+
+def vp_verify_drafts(logits, shard_offsets, global_max, global_sumexp, drafts, starts, uniforms, accepted, tokens, workspace, *,
+                     draft_logits=None, draft_max=None, draft_sumexp=None, stream=None) -> None:
+    """Verification of drafted tokens over the shards' logits ([N, rows] each) and the draw of the token behind them.  Sequence b
+    has the rows starts[b] .. starts[b + 1] - 1, one for each draft and a last one; draft_*: the draft model's, row by row, or
+    None (drafts that no model drew).  accepted [sequences] int32, tokens [N]: accepted drafts, the next token, -1 behind it."""
+    if not logits or any(t.dim() != 2 for t in logits):
+        raise VPError("logits must be [N, rows], a shard at least")
+    N, p = logits[0].shape[0], len(logits)
+    if len(shard_offsets) != p:
+        raise VPError("one offset per shard")
+    rows = [int(t.shape[1]) for t in logits]
+    shapes, dtype = [(N, n) for n in rows], (logits[0].dtype,)
+    if starts.dim() != 1 or starts.shape[0] < 2:
+        raise VPError("starts must be [sequences + 1], a sequence at least")
+    S = starts.shape[0] - 1
+    f, ids = (torch.float32,), (torch.int64,)
+    _on_current_device((*logits, global_max, global_sumexp, drafts, starts, uniforms, accepted, tokens, workspace,
+                        *(draft_logits or ()), draft_max, draft_sumexp))
+    wp, wb = _ws(workspace)
+    st = load_library().vp_verify_drafts(
+        _each(logits, "logits", dtype, shapes), _i64s(rows), _i64s(shard_offsets), p, _dtype_code(logits[0]),
+        _ptr(global_max, "global_max", f, (N,)), _ptr(global_sumexp, "global_sumexp", f, (N,)),
+        _each(draft_logits, "draft_logits", dtype, shapes), _ptr(draft_max, "draft_max", f, (N,)),
+        _ptr(draft_sumexp, "draft_sumexp", f, (N,)), _ptr(drafts, "drafts", ids, (N,)), _ptr(starts, "starts", ids),
+        _ptr(uniforms, "uniforms", f, (N,)), N, S, _ptr(accepted, "accepted", (torch.int32,), (S,)),
+        _ptr(tokens, "tokens", ids, (N,)), wp, wb, _stream(stream))
+    _check(st, "vp_verify_drafts")
 
 
 def vp_profile_mfma_loop(operands, out, iters: int, blocks: int, stream=None) -> None:

@@ -19,7 +19,8 @@ HOST = os.path.join(HERE, "_vphost.so")
 OBJDIR = os.path.join(HERE, "_build")
 
 SOURCES = ["vp_api.hip", "vp_profile.hip", "vp_gemm_bf16.hip", "vp_gemm_bf16_logits.hip", "vp_gemm_bf16_fast.hip", "vp_gemm_bf16_twin.hip", "vp_gemm_f32.hip", "vp_stats.hip", "vp_embed.hip",
-           "vp_block_norm.hip", "vp_block_norm_bwd_f32.hip", "vp_block_norm_bwd_bf16.hip", "vp_grad.hip"]
+           "vp_block_norm.hip", "vp_block_norm_bwd_f32.hip", "vp_block_norm_bwd_bf16.hip", "vp_grad.hip",
+           "vp_quantize.hip", "vp_gemm_i8.hip", "vp_verify.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

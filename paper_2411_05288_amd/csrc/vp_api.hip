@@ -1,5 +1,6 @@
 // extern "C" entry points of libvp: argument validation, workspace carving and the order of
 // kernel launches for each pass.  No allocation, no synchronisation, no state.
+#include <climits>
 #include <initializer_list>
 #include <mutex>
 
@@ -1058,6 +1059,181 @@ vp_status vp_grad_scale(const void* const* grads, const int64_t* counts, const i
                         float max_norm, const float* norm, void* workspace, size_t workspace_bytes, void* stream) {
     if (!(max_norm >= 0.f) || !finite(max_norm)) return VP_ERR_INVALID_ARG;
     return grad_call(grads, counts, dts, n, outs, max_norm, true, const_cast<float*>(norm), workspace, workspace_bytes, stream);
+}
+
+// ---- 8-bit integers
+
+int64_t vp_i8_row_stride(int64_t h) { return h < 1 || h > I8_MAX_ROW ? -1 : i8_row_stride(h); }
+
+vp_status vp_quantize_rows(const void* x, int64_t N, int64_t h, vp_dtype dt, int8_t* q, float* scales, void* stream) {
+    if (!x || !q || !scales || N < 1 || h < 1 || !dtype_ok(dt)) return VP_ERR_INVALID_ARG;
+    if (!aligned16(x) || !aligned16(q) || ((uintptr_t)scales & 3u)) return VP_ERR_INVALID_ARG;
+    if (h > I8_MAX_ROW || N >= MAX_ELEMS || N * i8_row_stride(h) >= MAX_ELEMS) return VP_ERR_UNSUPPORTED;
+    if (!outputs_apart({{x, (size_t)N * h * elem_bytes(dt)}}, {{q, (size_t)(N * i8_row_stride(h))}, {scales, (size_t)N * 4}}))
+        return VP_ERR_INVALID_ARG;
+    return dev(launch_quantize_rows(x, N, h, dt, q, scales, (hipStream_t)stream));
+}
+
+static bool i8_sizes_ok(int32_t p, int64_t N, const int64_t* rows) {
+    if (p < 1 || !rows || N < 1) return false;
+    for (int32_t r = 0; r < p; ++r)
+        if (!sizes_ok(N, 1, rows[r]) || !sizes_supported(N, 1, rows[r])) return false;
+    return true;
+}
+
+size_t vp_output_i8_workspace_bytes(int32_t p, int64_t N, const int64_t* rows) {
+    if (!i8_sizes_ok(p, N, rows)) return (size_t)-1;
+    size_t need = 0;
+    for (int32_t r0 = 0; r0 < p; r0 += GEMM_GROUP_MAX) {
+        const int n = p - r0 < GEMM_GROUP_MAX ? p - r0 : GEMM_GROUP_MAX;
+        int64_t tiles = 0;
+        for (int k = 0; k < n; ++k) tiles += fwd_tiles(rows[r0 + k]);
+        const size_t b = align_up((size_t)(2 * tiles + n) * N * sizeof(float), 256);
+        need = b > need ? b : need;
+    }
+    return need;
+}
+
+vp_status vp_output_fwd_i8_group(const int8_t* H, const float* H_scales, const int8_t* const* W_shards,
+                                 const float* const* W_scales, const int64_t* rows, const int64_t* shard_offsets, int32_t p,
+                                 const int64_t* labels, int64_t N, int64_t k, vp_dtype logits_dt, uint32_t flags,
+                                 float* local_max, float* local_sumexp, float* local_target, void* const* logits_out,
+                                 void* workspace, size_t workspace_bytes, void* stream) {
+    if (!H || !H_scales || !W_shards || !W_scales || !rows || !shard_offsets || p < 1 || !labels || !local_max ||
+        !local_sumexp || !local_target)
+        return VP_ERR_INVALID_ARG;
+    if (N < 1 || k < 1 || k % 128 || !dtype_ok(logits_dt) || (flags & ~(uint32_t)VP_SAVE_LOGITS)) return VP_ERR_INVALID_ARG;
+    if (((flags & VP_SAVE_LOGITS) != 0) != (logits_out != nullptr)) return VP_ERR_INVALID_ARG;
+    if (!aligned16(H) || !aligned16(workspace) || ((uintptr_t)labels & 7u)) return VP_ERR_INVALID_ARG;
+    if (((uintptr_t)H_scales | (uintptr_t)local_max | (uintptr_t)local_sumexp | (uintptr_t)local_target) & 3u) return VP_ERR_INVALID_ARG;
+    if (k > I8_MAX_ROW || N >= MAX_ELEMS || N * k >= MAX_ELEMS || (int64_t)p * N >= MAX_ELEMS) return VP_ERR_UNSUPPORTED;
+    for (int32_t r = 0; r < p; ++r) {
+        if (!W_shards[r] || !W_scales[r] || !aligned16(W_shards[r]) || ((uintptr_t)W_scales[r] & 3u)) return VP_ERR_INVALID_ARG;
+        if (rows[r] < 1 || shard_offsets[r] < 0) return VP_ERR_INVALID_ARG;
+        if (logits_out && (!logits_out[r] || !aligned16(logits_out[r]))) return VP_ERR_INVALID_ARG;
+        if (!sizes_supported(N, k, rows[r])) return VP_ERR_UNSUPPORTED;
+    }
+    const size_t need = vp_output_i8_workspace_bytes(p, N, rows);
+    if (!workspace || workspace_bytes < need) return VP_ERR_WORKSPACE;
+    // outputs: the statistics, the workspace, then the shards' logits
+    const size_t stats = (size_t)p * N * sizeof(float), elem = elem_bytes(logits_dt);
+    if (!outputs_apart({{H, (size_t)(N * k)}, {H_scales, (size_t)N * 4}, {labels, (size_t)N * 8}},
+                       {{local_max, stats}, {local_sumexp, stats}, {local_target, stats}, {workspace, need}}))
+        return VP_ERR_INVALID_ARG;
+    for (int32_t r = 0; r < p; ++r) {
+        const size_t own = logits_out ? (size_t)N * rows[r] * elem : 0;
+        if (!outputs_apart({{H, (size_t)(N * k)}, {H_scales, (size_t)N * 4}, {labels, (size_t)N * 8}, {local_max, stats},
+                            {local_sumexp, stats}, {local_target, stats}, {workspace, need}},
+                           {{logits_out ? logits_out[r] : nullptr, own}}))
+            return VP_ERR_INVALID_ARG;
+        for (int32_t i = 0; i < p; ++i) {
+            const Input w{W_shards[i], (size_t)(rows[i] * k)}, t{W_scales[i], (size_t)rows[i] * 4};
+            if (r == 0 && !outputs_apart({w, t}, {{local_max, stats}, {local_sumexp, stats}, {local_target, stats}, {workspace, need}}))
+                return VP_ERR_INVALID_ARG;
+            if (!logits_out) continue;
+            if (overlap(logits_out[r], own, w.p, w.bytes) || overlap(logits_out[r], own, t.p, t.bytes)) return VP_ERR_INVALID_ARG;
+            if (i < r && overlap(logits_out[r], own, logits_out[i], (size_t)N * rows[i] * elem)) return VP_ERR_INVALID_ARG;
+        }
+    }
+    hipStream_t st = (hipStream_t)stream;
+    for (int32_t r0 = 0; r0 < p; r0 += GEMM_GROUP_MAX) {
+        GemmI8Group g{};
+        ShardList l{};
+        l.n = g.n = p - r0 < GEMM_GROUP_MAX ? p - r0 : GEMM_GROUP_MAX;
+        g.H = H;
+        g.scales = H_scales;
+        g.labels = labels;
+        g.N = (int)N;
+        g.k = (int)k;
+        g.out_f32 = logits_dt == VP_F32;
+        for (int i = 0; i < GEMM_GROUP_MAX; ++i) {
+            g.first[i] = i < g.n ? g.total : INT_MAX;
+            if (i >= g.n) continue;
+            const int32_t r = r0 + i;
+            g.sh[i] = {W_shards[r], W_scales[r], logits_out ? logits_out[r] : nullptr, shard_offsets[r], (int)rows[r]};
+            l.rows[i] = (int)rows[r];
+            l.offset[i] = shard_offsets[r];
+            g.total += (int)fwd_tiles(rows[r]);
+            l.first[i + 1] = g.total;
+        }
+        g.part_max = (float*)workspace;
+        g.part_sum = g.part_max + (int64_t)g.total * N;
+        g.part_tgt = g.part_sum + (int64_t)g.total * N;
+        if (launch_gemm_i8(g, st) != hipSuccess ||
+            launch_fold_partials(g.part_max, g.part_sum, g.part_tgt, l, (int)N, labels, local_max + r0 * N, local_sumexp + r0 * N,
+                                 local_target + r0 * N, st) != hipSuccess)
+            return VP_ERR_DEVICE;
+    }
+    return VP_OK;
+}
+
+vp_status vp_output_fwd_i8(const int8_t* H, const float* H_scales, const int8_t* W_shard, const float* W_scales,
+                           const int64_t* labels, int64_t N, int64_t k, int64_t Vs, int64_t shard_offset, vp_dtype logits_dt,
+                           uint32_t flags, float* local_max, float* local_sumexp, float* local_target, void* logits_out,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+    return vp_output_fwd_i8_group(H, H_scales, &W_shard, &W_scales, &Vs, &shard_offset, 1, labels, N, k, logits_dt, flags,
+                                  local_max, local_sumexp, local_target, logits_out ? &logits_out : nullptr, workspace,
+                                  workspace_bytes, stream);
+}
+
+// ---- verification of drafts
+
+size_t vp_verify_workspace_bytes(int32_t sequences, int64_t V) {
+    return sequences < 1 || V < 1 || V >= MAX_ELEMS ? (size_t)-1 : verify_workspace(sequences, V);
+}
+
+vp_status vp_verify_drafts(const void* const* logits, const int64_t* rows, const int64_t* shard_offsets, int32_t p, vp_dtype dt,
+                           const float* global_max, const float* global_sumexp, const void* const* draft_logits,
+                           const float* draft_max, const float* draft_sumexp, const int64_t* drafts, const int64_t* starts,
+                           const float* uniforms, int64_t N, int32_t sequences, int32_t* accepted, int64_t* tokens,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+    if (!logits || !rows || !shard_offsets || p < 1 || !dtype_ok(dt) || !global_max || !global_sumexp || !drafts || !starts ||
+        !uniforms || N < 1 || sequences < 1 || !accepted || !tokens)
+        return VP_ERR_INVALID_ARG;
+    if ((draft_logits != nullptr) != (draft_max != nullptr) || (draft_logits != nullptr) != (draft_sumexp != nullptr))
+        return VP_ERR_INVALID_ARG;
+    if (((uintptr_t)global_max | (uintptr_t)global_sumexp | (uintptr_t)draft_max | (uintptr_t)draft_sumexp | (uintptr_t)uniforms |
+         (uintptr_t)accepted) & 3u)
+        return VP_ERR_INVALID_ARG;
+    if ((((uintptr_t)drafts | (uintptr_t)starts | (uintptr_t)tokens) & 7u) || !aligned16(workspace)) return VP_ERR_INVALID_ARG;
+    if (p > VERIFY_MAX_SHARDS || N >= MAX_ELEMS) return VP_ERR_UNSUPPORTED;
+    int64_t V = 0;
+    for (int32_t r = 0; r < p; ++r) {
+        if (!logits[r] || ((uintptr_t)logits[r] & (elem_bytes(dt) - 1)) || rows[r] < 1 || shard_offsets[r] < 0 || shard_offsets[r] > INT64_MAX - rows[r])
+            return VP_ERR_INVALID_ARG;
+        if (draft_logits && (!draft_logits[r] || ((uintptr_t)draft_logits[r] & (elem_bytes(dt) - 1)))) return VP_ERR_INVALID_ARG;
+        if (!sizes_supported(N, 1, rows[r])) return VP_ERR_UNSUPPORTED;
+        for (int32_t i = 0; i < r; ++i)
+            if (shard_offsets[i] < shard_offsets[r] + rows[r] && shard_offsets[r] < shard_offsets[i] + rows[i]) return VP_ERR_INVALID_ARG;
+        V += rows[r];
+    }
+    const size_t need = vp_verify_workspace_bytes(sequences, V);
+    if (!workspace || workspace_bytes < need) return VP_ERR_WORKSPACE;
+    const size_t n4 = (size_t)N * 4, n8 = (size_t)N * 8;
+    const Output a{accepted, (size_t)sequences * 4}, t{tokens, n8}, w{workspace, need};
+    if (!outputs_apart({{global_max, n4}, {global_sumexp, n4}, {draft_max, n4}, {draft_sumexp, n4}, {drafts, n8},
+                        {starts, ((size_t)sequences + 1) * 8}, {uniforms, n4}},
+                       {a, t, w}))
+        return VP_ERR_INVALID_ARG;
+    Verify v{};
+    for (int32_t r = 0; r < p; ++r) {
+        const size_t bytes = (size_t)N * rows[r] * elem_bytes(dt);
+        if (!outputs_apart({{logits[r], bytes}, {draft_logits ? draft_logits[r] : nullptr, bytes}}, {a, t, w})) return VP_ERR_INVALID_ARG;
+        v.sh[r] = {logits[r], draft_logits ? draft_logits[r] : nullptr, shard_offsets[r], (int)rows[r], 0};
+    }
+    v.p = p;
+    v.sequences = sequences;
+    v.N = N;
+    v.gmax = global_max;
+    v.gsum = global_sumexp;
+    v.zmax = draft_max;
+    v.zsum = draft_sumexp;
+    v.drafts = drafts;
+    v.starts = starts;
+    v.uniforms = uniforms;
+    v.accepted = accepted;
+    v.tokens = tokens;
+    return dev(launch_verify(v, dt, workspace, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -19,7 +19,7 @@ static inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; 
 enum KernelId : int {
     K_GEMM_FWD_STATS = 0, K_GEMM_DLOGITS, K_GEMM_DH, K_GEMM_DW, K_FOLD, K_COMBINE, K_DLOGITS_EW, K_GEMM_F32,
     K_ROWSTATS_F32, K_EMBED_FWD, K_EMBED_SORT, K_EMBED_ACCUM, K_GEMM_A_ALG2, K_DX_ALG2, K_SUM_SLICES, K_ZERO_PAD,
-    K_BLOCK_NORM_FWD, K_BLOCK_NORM_BWD, K_GRAD_NORM, K_GRAD_SCALE, K_COUNT
+    K_BLOCK_NORM_FWD, K_BLOCK_NORM_BWD, K_GRAD_NORM, K_GRAD_SCALE, K_QUANTIZE, K_GEMM_I8, K_VERIFY, K_COUNT
 };
 
 // Brackets the launches made during its lifetime with two events when timing is enabled;
@@ -263,5 +263,51 @@ hipError_t launch_block_norm_bwd(const BlockNormGrad& p, vp_dtype dt, vp_dtype d
 size_t grad_workspace(int32_t n);
 hipError_t launch_grad(const void* const* grads, const int64_t* counts, const int32_t* dts, int32_t n, void* const* outs,
                        float max_norm, bool known, float* norm, void* workspace, hipStream_t st);
+
+// 8-bit rows: bytes of a row of h elements, and the most a row may have.
+constexpr int64_t I8_MAX_ROW = ((int64_t)1 << 17) - 128;
+static inline int64_t i8_row_stride(int64_t h) { return (h + 127) / 128 * 128; }
+hipError_t launch_quantize_rows(const void* x, int64_t N, int64_t h, vp_dtype dt, int8_t* q, float* scales, hipStream_t st);
+
+// The logits product of 8-bit integers over up to GEMM_GROUP_MAX shards, with its statistics (partials as in GemmBf16Params).
+struct GemmI8Shard {
+    const int8_t* W;
+    const float* scales;
+    void* out;           // [N, rows], or nullptr
+    int64_t offset;
+    int rows;
+};
+struct GemmI8Group {
+    const int8_t* H;
+    const float* scales;
+    const int64_t* labels;
+    int N, k;
+    int out_f32;         // type of the logits that are kept
+    float *part_max, *part_sum, *part_tgt;
+    int n, total;                  // shards; tile columns of all of them
+    int first[GEMM_GROUP_MAX];     // first tile column of shard r (INT_MAX from n on)
+    GemmI8Shard sh[GEMM_GROUP_MAX];
+};
+hipError_t launch_gemm_i8(const GemmI8Group& g, hipStream_t st);
+
+// Verification of drafts: see vp.h.
+constexpr int VERIFY_MAX_SHARDS = 64;
+struct VerifyShard {
+    const void *Y, *Z;
+    int64_t offset;
+    int rows, first;     // first chunk
+};
+struct Verify {
+    VerifyShard sh[VERIFY_MAX_SHARDS];
+    int p, sequences;
+    int64_t N;
+    const float *gmax, *gsum, *zmax, *zsum;
+    const int64_t *drafts, *starts;
+    const float* uniforms;
+    int32_t* accepted;
+    int64_t* tokens;
+};
+size_t verify_workspace(int64_t sequences, int64_t V);
+hipError_t launch_verify(const Verify& v, vp_dtype dt, void* workspace, hipStream_t st);
 
 }  // namespace vp

@@ -352,6 +352,118 @@ class OutputLayerPlan:
                                  self.dH, self.dW, self.logits)
 
 
+def _on(stream):
+    """Context in which torch's own work runs on the same stream as the library's kernels."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream))
+    return torch.cuda.stream(stream)
+
+
+def quantize_rows(x: torch.Tensor, stream=None):
+    """The rows of x in 8-bit integers, and their scales: what OutputLayerI8Plan takes for a shard of the weights."""
+    if x.dim() != 2:
+        raise B.VPError("x must be [rows, h]")
+    with _on(stream):
+        q = torch.empty((x.shape[0], B.vp_i8_row_stride(x.shape[1])), dtype=torch.int8, device=x.device)
+        scales = torch.empty((x.shape[0],), dtype=torch.float32, device=x.device)
+    B.vp_quantize_rows(x, q, scales, stream)
+    return q, scales
+
+
+class OutputLayerI8Plan:
+    """The output layer's logits and statistics with weights and hidden states in 8-bit integers, for answering and scoring: there
+    is no backward pass.  ``W_shards`` are pairs of integers and scales (``quantize_rows`` of a shard, made once and shared by
+    plans of all sizes); the rows of H become integers in every pass.  Shards, padding (``vocab_size``) and ``norm`` are those of
+    OutputLayerPlan.  Without ``labels`` loss and target logits stand for nothing.  ``logits`` are kept (``save_logits``) in
+    ``logits_dtype``, by default that of H: what DraftVerifyPlan draws tokens from."""
+
+    def __init__(self, H: Optional[torch.Tensor], W_shards, labels: Optional[torch.Tensor] = None, *, save_logits: bool = True,
+                 logits_dtype: Optional[torch.dtype] = None, vocab_size: Optional[int] = None,
+                 norm: Optional[BlockNormPlan] = None):
+        if (H is None) == (norm is None):
+            raise B.VPError("either H or the norm that makes it")
+        H = norm.H if H is None else H
+        if H.dim() != 2:
+            raise B.VPError("H must be [N, h]")
+        self.H, self.norm = H, norm
+        self.N, self.h = H.shape
+        stride = B.vp_i8_row_stride(self.h)
+        offset, total = 0, sum(int(q.shape[0]) for q, _ in W_shards)
+        self.vocab_size = total if vocab_size is None else int(vocab_size)
+        if not 0 < self.vocab_size <= total:
+            raise B.VPError("vocab_size must be in (0, total rows]")
+        self.W, self.W_scales, self.offsets, self.valid = [], [], [], []      # of the shards with real rows
+        for q, scales in W_shards:
+            rows, valid = int(q.shape[0]), max(0, min(int(q.shape[0]), self.vocab_size - offset))
+            if q.dim() != 2 or q.shape[1] != stride or scales.shape != (rows,):
+                raise B.VPError("every shard must be ([rows, %d] integers, [rows] scales)" % stride)
+            if valid > 0:
+                self.W.append(q if valid == rows else q[:valid])
+                self.W_scales.append(scales if valid == rows else scales[:valid])
+                self.offsets.append(offset)
+                self.valid.append(valid)
+            offset += rows
+        self.p = len(self.W)
+        dev = H.device
+        f32 = dict(dtype=torch.float32, device=dev)
+        self.labels = torch.full((self.N,), -1, dtype=torch.int64, device=dev) if labels is None else labels
+        self.H_i8 = torch.empty((self.N, stride), dtype=torch.int8, device=dev)
+        self.H_scales = torch.empty((self.N,), **f32)
+        self.local_max, self.local_sumexp, self.local_target = (torch.empty((self.p, self.N), **f32) for _ in range(3))
+        self.global_max, self.global_sumexp, self.loss_rows = (torch.empty((self.N,), **f32) for _ in range(3))
+        self.loss = torch.empty((1,), **f32)
+        self.logits = ([torch.empty((self.N, v), dtype=logits_dtype or H.dtype, device=dev) for v in self.valid]
+                       if save_logits else None)
+        self.workspace = torch.empty((B.vp_output_i8_workspace_bytes(self.N, self.valid),), dtype=torch.uint8, device=dev)
+
+    def forward(self, stream=None) -> None:
+        if self.norm is not None:
+            self.norm.forward(stream)
+        B.vp_quantize_rows(self.H, self.H_i8, self.H_scales, stream)
+        B.vp_output_fwd_i8_group(self.H_i8, self.H_scales, self.W, self.W_scales, self.labels, self.offsets, self.local_max,
+                                 self.local_sumexp, self.local_target, self.logits, self.workspace, stream)
+        B.vp_combine_stats(self.local_max, self.local_sumexp, self.local_target, self.global_max, self.global_sumexp,
+                           self.loss_rows, self.loss, stream)
+
+
+class DraftVerifyPlan:
+    """Verification of drafted tokens against the logits that ``target`` keeps (an OutputLayerPlan or OutputLayerI8Plan), and the
+    draw of the token behind them.  Sequence b has the rows starts[b] .. starts[b + 1] - 1 of the target's tokens, one for each
+    of its drafts and a last one; ``drafts`` [N] holds the token that each row is asked about, ``uniforms`` [N] random numbers in
+    [0, 1).  ``draft``: the plan of the model that drew the drafts, with the same shards and rows (its last rows are not read),
+    or None.  Results: ``accepted`` [sequences], ``tokens`` [N]."""
+
+    def __init__(self, target, starts: torch.Tensor, drafts: torch.Tensor, uniforms: torch.Tensor, draft=None):
+        if target.logits is None or (draft is not None and draft.logits is None):
+            raise B.VPError("plans whose logits are drawn from keep them (save_logits)")
+        self.target, self.draft = target, draft
+        self.starts, self.drafts, self.uniforms = starts, drafts, uniforms
+        self.logits, self.offsets = self._shards(target)
+        self.draft_logits = None
+        if draft is not None:
+            self.draft_logits, offsets = self._shards(draft)
+            if offsets != self.offsets or [t.shape for t in self.logits] != [t.shape for t in self.draft_logits]:
+                raise B.VPError("the plans of the target and of the draft model have the same shards and rows")
+        V, sequences = sum(int(t.shape[1]) for t in self.logits), starts.shape[0] - 1
+        self.accepted = torch.empty((max(sequences, 0),), dtype=torch.int32, device=starts.device)
+        self.tokens = torch.empty((target.N,), dtype=torch.int64, device=starts.device)
+        self.workspace = torch.empty((B.vp_verify_workspace_bytes(sequences, V),), dtype=torch.uint8, device=starts.device)
+
+    @staticmethod
+    def _shards(plan):
+        live = [r for r, v in enumerate(plan.valid) if v > 0]
+        return [plan.logits[r] for r in live], [plan.offsets[r] for r in live]
+
+    def forward(self, stream=None) -> None:
+        d = self.draft
+        B.vp_verify_drafts(self.logits, self.offsets, self.target.global_max, self.target.global_sumexp, self.drafts, self.starts,
+                           self.uniforms, self.accepted, self.tokens, self.workspace, draft_logits=self.draft_logits,
+                           draft_max=None if d is None else d.global_max, draft_sumexp=None if d is None else d.global_sumexp,
+                           stream=stream)
+
+
 def output_layer_step(H, W_shards, labels, save_logits=True, grad_scale=None, vocab_size=None) -> OutputLayerResult:
     """One forward + backward of the sharded output layer; returns all outputs."""
     plan = OutputLayerPlan(H, W_shards, labels, save_logits, grad_scale, vocab_size)

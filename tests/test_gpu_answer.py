@@ -1,0 +1,207 @@
+"""The operators that answer, together as they are used: a norm, hidden states and weights in 8-bit integers, logits and statistics of
+the shards, drafted tokens verified against them."""
+import numpy as np
+import pytest
+import torch
+
+import answer_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def weights(rows, h, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    return [(torch.randn(n, h, generator=gen, device="cuda") * 0.05).to(torch.bfloat16) for n in rows]
+
+
+class Model:
+    """The end of a model: a norm and the output layer in integers."""
+
+    def __init__(self, N, h, rows, seed, vocab_size=None, logits_dtype=None, labels=None):
+        import paper_2411_05288_amd as vp
+        self.x = torch.randn(N, h, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda").to(torch.bfloat16)
+        self.W = weights(rows, h, seed + 1)
+        self.norm = vp.BlockNormPlan(self.x, w=torch.ones(h, dtype=torch.bfloat16, device="cuda"), train=False)
+        self.plan = vp.OutputLayerI8Plan(None, [vp.quantize_rows(w) for w in self.W], labels, norm=self.norm,
+                                         vocab_size=vocab_size, logits_dtype=logits_dtype)
+
+    def reference(self):
+        """Logits and statistics in 64 bits of the plan's own normed states."""
+        qH, sH = ref.quantize_rows_fast(self.norm.H.double().cpu().numpy())
+        V = self.plan.vocab_size
+        qW, sW = ref.quantize_rows_fast(torch.cat(self.W)[:V].double().cpu().numpy())
+        Y = ref.logits(qH, sH, qW, sW)
+        return Y, Y.max(1), np.exp(Y - Y.max(1, keepdims=True)).sum(1)
+
+
+def inputs(counts, V, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    starts = torch.tensor(np.concatenate([[0], np.cumsum([c + 1 for c in counts])]), device="cuda")
+    N = int(starts[-1])
+    return starts, torch.randint(0, V, (N,), generator=gen, device="cuda"), torch.rand(N, generator=gen, device="cuda")
+
+
+def check(verify, order):
+    """The verification against the definition, on the logits and statistics that the plans left."""
+    host = lambda t: None if t is None else t.cpu().numpy()      # noqa: E731
+    joined = lambda ts: None if ts is None else torch.cat([t.double() for t in ts], 1).cpu().numpy()      # noqa: E731
+    t, d = verify.target, verify.draft
+    a, tokens, margins = ref.verify(joined(verify.logits), host(t.global_max), host(t.global_sumexp), host(verify.drafts),
+                                    host(verify.starts), host(verify.uniforms), np.full(t.N, -5), order, joined(verify.draft_logits),
+                                    None if d is None else host(d.global_max), None if d is None else host(d.global_sumexp))
+    assert (margins > 1e-12).all()
+    np.testing.assert_array_equal(host(verify.accepted), a)
+    np.testing.assert_array_equal(host(verify.tokens), tokens)
+
+
+@pytest.mark.parametrize("logits_dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,vocab_size", [([300, 300, 300], 900), ([300, 300, 300], 501), ([300, 300, 300], 300), ([700], 650)])
+def test_a_step_of_an_answer(rows, vocab_size, logits_dtype):
+    import paper_2411_05288_amd as vp
+    counts = [3, 0, 5, 1]
+    N, h = sum(counts) + len(counts), 200
+    labels = torch.randint(0, vocab_size, (N,), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    target, draft = (Model(N, h, rows, s, vocab_size, logits_dtype, labels) for s in (1, 5))
+    starts, _, uniforms = inputs(counts, vocab_size, 3)
+    draft.plan.forward()
+    drafts = torch.cat(draft.plan.logits, 1).float().argmax(1)
+    verify = vp.DraftVerifyPlan(target.plan, starts, drafts, uniforms, draft=draft.plan)
+    target.plan.forward()
+    verify.forward()
+    torch.cuda.synchronize()
+    check(verify, np.arange(vocab_size))
+    for model in (target, draft):
+        Y, m, s = model.reference()
+        p = model.plan
+        A = np.abs(Y).max()
+        # (bounds of the logits, the statistics of a shard and their sum as in the tests of the product)
+        assert np.abs(p.global_max.cpu().numpy() - m).max() <= 4 * 2.0 ** -24 * A
+        loss = np.log(s) + m - Y[np.arange(N), labels.cpu().numpy()]
+        tol = 2.0 ** -24 * (48 * A + 400)
+        assert np.abs(p.loss_rows.cpu().numpy() - loss).max() <= tol + 2.0 ** -22 * np.abs(loss).max()
+        assert abs(p.loss.item() - loss.mean()) <= tol + 2.0 ** -21 * np.abs(loss).max()
+
+
+def test_a_plan_without_labels_and_one_token():
+    import paper_2411_05288_amd as vp
+    W = [vp.quantize_rows(w) for w in weights([500, 400], 129, 3)]
+    H = torch.randn(1, 129, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")
+    plan = vp.OutputLayerI8Plan(H, W)
+    assert plan.logits[0].dtype == torch.float32
+    starts, drafts, uniforms = inputs([0], 900, 1)
+    verify = vp.DraftVerifyPlan(plan, starts, drafts, uniforms)
+    plan.forward()
+    verify.forward()
+    torch.cuda.synchronize()
+    check(verify, np.arange(900))
+
+
+@pytest.mark.parametrize("algorithm", [1, 2])
+def test_verification_over_the_trained_layers_logits(algorithm):
+    """The logits and statistics of OutputLayerPlan, with shards of padding behind the vocabulary."""
+    import paper_2411_05288_amd as vp
+    counts, rows, h, V = [2, 4, 0, 3], [128, 128, 128, 128], 64, 300
+    N = sum(counts) + len(counts)
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    plans = []
+    for seed in (1, 2):
+        H = torch.randn(N, h, generator=gen, device="cuda").to(torch.bfloat16)
+        plans.append(vp.OutputLayerPlan(H, weights(rows, h, seed), torch.zeros(N, dtype=torch.int64, device="cuda"), vocab_size=V,
+                                        algorithm=algorithm))
+        plans[-1].forward()
+    starts, drafts, uniforms = inputs(counts, V, 9)
+    verify = vp.DraftVerifyPlan(plans[0], starts, drafts, uniforms, draft=plans[1])
+    verify.forward()
+    torch.cuda.synchronize()
+    check(verify, np.arange(V))
+
+
+def test_refusals_of_the_plans():
+    import paper_2411_05288_amd as vp
+    W = [vp.quantize_rows(w) for w in weights([64, 64], 100, 1)]
+    H = torch.zeros(3, 100, device="cuda")
+    starts, drafts, uniforms = inputs([2], 128, 1)
+    for bad in (dict(H=None), dict(H=torch.zeros(100, device="cuda")), dict(H=torch.zeros(3, 200, device="cuda")), dict(vocab_size=0),
+                dict(vocab_size=129), dict(W_shards=[(W[0][0], W[1][1][:5])]), dict(W_shards=[(W[0][0].view(-1), W[0][1])])):
+        with pytest.raises(vp.VPError):
+            vp.OutputLayerI8Plan(**{**dict(H=H, W_shards=W), **bad})
+    alone, plan = vp.OutputLayerI8Plan(H, W, save_logits=False), vp.OutputLayerI8Plan(H, W)
+    other = vp.OutputLayerI8Plan(H, W[:1])
+    for a, k in (((alone,), {}), ((plan,), dict(draft=alone)), ((plan,), dict(draft=other))):
+        with pytest.raises(vp.VPError):
+            vp.DraftVerifyPlan(*a, starts, drafts, uniforms, **k)
+    with pytest.raises(vp.VPError):
+        vp.quantize_rows(torch.zeros(4, device="cuda"))
+
+
+def step_of(target, draft, verify):
+    draft.plan.forward()
+    target.plan.forward()
+    verify.forward()
+
+
+def test_a_step_in_a_graph_and_on_another_stream():
+    """Captured once and replayed with other inputs in the same buffers, with the program's own work in between; two graphs of two
+    plans replayed in turn; the same through a stream argument."""
+    import paper_2411_05288_amd as vp
+    counts, rows, h = [3, 0, 5, 1, 2], [300, 400], 256
+    N = sum(counts) + len(counts)
+    runs = []
+    for seed in (1, 20):
+        target, draft = Model(N, h, rows, seed), Model(N, h, rows, seed + 5)
+        starts, drafts, uniforms = inputs(counts, 700, seed)
+        verify = vp.DraftVerifyPlan(target.plan, starts, drafts, uniforms, draft=draft.plan)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            step_of(target, draft, verify)
+        torch.cuda.current_stream().wait_stream(side)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step_of(target, draft, verify)
+        runs.append((target, draft, verify, graph))
+    gen = torch.Generator(device="cuda").manual_seed(99)
+    for turn in range(4):
+        want = []
+        for target, draft, verify, graph in runs:
+            target.x.copy_(torch.randn(N, h, generator=gen, device="cuda"))
+            draft.x.copy_(target.x.float() + 0.3 * torch.randn(N, h, generator=gen, device="cuda"))
+            verify.uniforms.copy_(torch.rand(N, generator=gen, device="cuda"))
+            verify.drafts.copy_(torch.randint(0, 700, (N,), generator=gen, device="cuda"))
+            step_of(target, draft, verify)
+            torch.cuda.synchronize()
+            check(verify, np.arange(700))
+            want.append([t.clone() for t in (verify.accepted, verify.tokens, target.plan.loss_rows, *target.plan.logits)])
+            verify.tokens.fill_(-9)
+            target.plan.workspace.fill_(0xFF)
+            verify.workspace.fill_(0xFF)
+        for _, _, _, graph in runs:
+            graph.replay()
+        torch.cuda.synchronize()
+        assert float(torch.arange(1000, device="cuda", dtype=torch.float32).sum()) == 499500.0
+        for (target, _, verify, _), w in zip(runs, want):
+            for a, b in zip((verify.accepted, verify.tokens, target.plan.loss_rows, *target.plan.logits), w):
+                assert torch.equal(a, b)
+        stream = torch.cuda.Stream()
+        stream.wait_stream(torch.cuda.current_stream())
+        for argument in (stream, stream.cuda_stream):
+            for (target, draft, verify, _), w in zip(runs, want):
+                verify.tokens.fill_(-9)
+                stream.wait_stream(torch.cuda.current_stream())
+                for p in (draft.plan, target.plan, verify):
+                    p.forward(argument)
+                stream.synchronize()
+                assert torch.equal(verify.tokens, w[1]) and torch.equal(verify.accepted, w[0])
+
+
+def test_rows_become_integers_on_another_stream():
+    import paper_2411_05288_amd as vp
+    w = weights([700], 300, 1)[0]
+    a = vp.quantize_rows(w)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    b = vp.quantize_rows(w, stream)
+    c = vp.quantize_rows(w, stream.cuda_stream)
+    stream.synchronize()
+    for t in (b, c):
+        assert torch.equal(a[0], t[0]) and torch.equal(a[1], t[1])
