@@ -1,6 +1,5 @@
 // extern "C" entry points of libvp: argument validation, workspace carving and the order of
 // kernel launches for each pass.  No allocation, no synchronisation, no state.
-#include <climits>
 #include <initializer_list>
 #include <mutex>
 
@@ -1139,29 +1138,29 @@ vp_status vp_output_fwd_i8_group(const int8_t* H, const float* H_scales, const i
     for (int32_t r0 = 0; r0 < p; r0 += GEMM_GROUP_MAX) {
         GemmI8Group g{};
         ShardList l{};
-        l.n = g.n = p - r0 < GEMM_GROUP_MAX ? p - r0 : GEMM_GROUP_MAX;
-        g.H = H;
-        g.scales = H_scales;
-        g.labels = labels;
-        g.N = (int)N;
-        g.k = (int)k;
+        const int n = p - r0 < GEMM_GROUP_MAX ? p - r0 : GEMM_GROUP_MAX;
+        l.n = n;
+        g.base = logits_product(H, labels, N, k / 2, Epi::LogitsI8);
+        g.base.kernel_id = K_GEMM_I8;
+        g.row_scales = H_scales;
         g.out_f32 = logits_dt == VP_F32;
-        for (int i = 0; i < GEMM_GROUP_MAX; ++i) {
-            g.first[i] = i < g.n ? g.total : INT_MAX;
-            if (i >= g.n) continue;
+        for (int i = 0; i < n; ++i) {
             const int32_t r = r0 + i;
-            g.sh[i] = {W_shards[r], W_scales[r], logits_out ? logits_out[r] : nullptr, shard_offsets[r], (int)rows[r]};
-            l.rows[i] = (int)rows[r];
-            l.offset[i] = shard_offsets[r];
-            g.total += (int)fwd_tiles(rows[r]);
-            l.first[i + 1] = g.total;
+            g.sh[i].B = (const u16*)W_shards[r];
+            g.sh[i].out = logits_out ? logits_out[r] : nullptr;
+            g.sh[i].ld = g.sh[i].rows = l.rows[i] = (int)rows[r];
+            g.sh[i].offset = l.offset[i] = shard_offsets[r];
+            g.col_scales[i] = W_scales[r];
+            l.first[i + 1] = l.first[i] + (int)fwd_tiles(rows[r]);
         }
-        g.part_max = (float*)workspace;
-        g.part_sum = g.part_max + (int64_t)g.total * N;
-        g.part_tgt = g.part_sum + (int64_t)g.total * N;
+        gemm_bf16_group_finish(g, n);
+        float* pm = (float*)workspace;
+        g.base.part_max = pm;
+        g.base.part_sum = pm + (int64_t)g.total * N;
+        g.base.part_tgt = pm + 2 * (int64_t)g.total * N;
         if (launch_gemm_i8(g, st) != hipSuccess ||
-            launch_fold_partials(g.part_max, g.part_sum, g.part_tgt, l, (int)N, labels, local_max + r0 * N, local_sumexp + r0 * N,
-                                 local_target + r0 * N, st) != hipSuccess)
+            launch_fold_partials(g.base.part_max, g.base.part_sum, g.base.part_tgt, l, (int)N, labels, local_max + r0 * N,
+                                 local_sumexp + r0 * N, local_target + r0 * N, st) != hipSuccess)
             return VP_ERR_DEVICE;
     }
     return VP_OK;

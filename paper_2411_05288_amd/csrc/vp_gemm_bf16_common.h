@@ -23,6 +23,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
+typedef int intx4 __attribute__((ext_vector_type(4)));
+typedef int intx16 __attribute__((ext_vector_type(16)));
 
 constexpr int BM = GEMM_BM, BN = GEMM_BN, BK = 64;
 constexpr int NT = 256;   // threads per workgroup
@@ -43,7 +45,11 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // acc[i][j] += A-rows(i) x B-rows(j), stored transposed (see the layout above)
 template <Epi EPI>
 __device__ __forceinline__ void mfma_tile(floatx16& c, const bf16x8& a, const bf16x8& b) {
-    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, a, c, 0, 0, 0);
+    if constexpr (EPI == Epi::LogitsI8)      // 16 integers in place of 8 numbers; the accumulators hold integers
+        c = __builtin_bit_cast(floatx16, __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(intx4, b), __builtin_bit_cast(intx4, a),
+                                                                              __builtin_bit_cast(intx16, c), 0, 0, 0));
+    else
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, a, c, 0, 0, 0);
 }
 
 // Pass S, ragged last column tile: the accumulators of the columns past the end of the shard are

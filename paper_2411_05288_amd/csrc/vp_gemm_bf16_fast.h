@@ -35,6 +35,7 @@
 #pragma once
 
 #include "vp_gemm_bf16_common.h"
+#include "vp_gemm_i8_epilogue.h"
 
 namespace vp {
 
@@ -223,8 +224,8 @@ __device__ __forceinline__ int shard_of(const GemmBf16Group& gg, int t) {
 // MI: row blocks of 32 per wavefront, tiles of 64 MI rows (row_blocks_for); A's half of a slot then holds 64 MI rows.  Up to 256
 // tokens the logits products and dH are bound by reading W (N=64 h=4096 V=64000: 97 us, 5.4 TB/s), if the matrix work of a
 // k tile and the loads of A stay below that.
-template <bool A_KC, bool B_KC, Epi EPI, bool STREAM, bool TRACE, bool KTAIL, int MI = 4>
-__global__ __launch_bounds__(NT) void gemm_bf16_fast_kernel(GemmBf16Group gg) {
+template <bool A_KC, bool B_KC, Epi EPI, bool STREAM, bool TRACE, bool KTAIL, int MI = 4, typename Group = GemmBf16Group>
+__global__ __launch_bounds__(NT) void gemm_bf16_fast_kernel(Group gg) {
     constexpr int TM = 64 * MI;
     static_assert(MI == 4 || A_KC, "the K-strided layout has 256 rows");
     constexpr bool CAT_N = A_KC && B_KC, CAT_M = !A_KC && !B_KC, CAT_K = A_KC && !B_KC;
@@ -321,6 +322,8 @@ __global__ __launch_bounds__(NT) void gemm_bf16_fast_kernel(GemmBf16Group gg) {
         half_voffsets<B_KC>(bvoff, n0, g.ldb, wave, lane);
     };
     bind_shard();
+    I8Inputs i8;      // asked for here: in the epilogue they would be waited for
+    if constexpr (EPI == Epi::LogitsI8) i8.load(g, gg.row_scales, gg.col_scales[shard], m0, n0, cols_n);
 
     // Instruction-mix hints for the scheduler: the next N MFMAs, LDS reads, global loads.
 #define VP_SCHED_MFMA(n) __builtin_amdgcn_sched_group_barrier(0x008, n, 0)
@@ -484,7 +487,7 @@ __global__ __launch_bounds__(NT) void gemm_bf16_fast_kernel(GemmBf16Group gg) {
             e.Y = (u16*)s.out;
             e.ldy = s.ld;
             e.shard_offset = s.offset;
-            if constexpr (EPI == Epi::FwdStats) {
+            if constexpr (EPI == Epi::FwdStats || EPI == Epi::LogitsI8) {
                 e.part_max = g.part_max + (size_t)gg.first[shard] * g.M;
                 e.part_sum = g.part_sum + (size_t)gg.first[shard] * g.M;
                 e.part_tgt = g.part_tgt + (size_t)shard * g.M;
@@ -497,8 +500,9 @@ __global__ __launch_bounds__(NT) void gemm_bf16_fast_kernel(GemmBf16Group gg) {
         }
     }
     // exchange area at the start of slot 0; staging block of wavefront w in slot w (behind the exchange area in slot 0)
-    gemm_epilogue<EPI, 4, 2, STREAM, MI>(acc, e, tile_m, tile_n, g_slot0,
-                                     wave == 0 ? g_slot0 + EPI_XCHG_BYTES : wave == 1 ? g_slot1 : wave == 2 ? g_slot2 : g_slot3);
+    char* region = wave == 0 ? g_slot0 + EPI_XCHG_BYTES : wave == 1 ? g_slot1 : wave == 2 ? g_slot2 : g_slot3;
+    if constexpr (EPI == Epi::LogitsI8) gemm_epilogue_i8<STREAM, MI>(acc, e, gg.out_f32, i8, tile_m, tile_n, g_slot0, region);
+    else gemm_epilogue<EPI, 4, 2, STREAM, MI>(acc, e, tile_m, tile_n, g_slot0, region);
     __syncthreads();   // the epilogue's LDS exchange is over before the next tile streams in
     trace_stamp<TRACE>(g, tile_idx, 3);
     }   // persistent tile loop
@@ -512,19 +516,20 @@ unsigned long long* gemm_bf16_trace_buffer(int kernel_id, size_t& words);
 int row_blocks_for(int64_t M, int64_t tn, int64_t kt, bool stats, int cus);
 
 // One instantiation's launch.
-template <bool A_KC, bool B_KC, Epi EPI, int MI, bool KTAIL>
-static void launch_tiles(const GemmBf16Group& p, int tiles, int cus, hipStream_t st) {
+template <bool A_KC, bool B_KC, Epi EPI, int MI, bool KTAIL, typename Group>
+static void launch_tiles(const Group& p, int tiles, int cus, hipStream_t st) {
     // more tiles than workgroups: outputs are streamed past the L2 (see gemm_epilogue)
     if (tiles > cus)
-        hipLaunchKernelGGL((gemm_bf16_fast_kernel<A_KC, B_KC, EPI, true, false, KTAIL, MI>), dim3(cus), dim3(NT), 0, st, p);
+        hipLaunchKernelGGL((gemm_bf16_fast_kernel<A_KC, B_KC, EPI, true, false, KTAIL, MI, Group>), dim3(cus), dim3(NT), 0, st, p);
     else
-        hipLaunchKernelGGL((gemm_bf16_fast_kernel<A_KC, B_KC, EPI, false, false, KTAIL, MI>), dim3(tiles), dim3(NT), 0, st, p);
+        hipLaunchKernelGGL((gemm_bf16_fast_kernel<A_KC, B_KC, EPI, false, false, KTAIL, MI, Group>), dim3(tiles), dim3(NT), 0, st, p);
 }
 
-template <bool A_KC, bool B_KC, Epi EPI>
-static hipError_t launch_fast_t(const GemmBf16Group& p0, hipStream_t st) {
-    GemmBf16Group p = p0;
-    const bool cat_k = A_KC && !B_KC, ktail = A_KC && B_KC && p.base.K % BK != 0;
+template <bool A_KC, bool B_KC, Epi EPI, typename Group>
+static hipError_t launch_fast_t(const Group& p0, hipStream_t st) {
+    Group p = p0;
+    constexpr bool KTAILS = A_KC && B_KC && EPI != Epi::LogitsI8;      // (rows of integers are padded)
+    const bool cat_k = A_KC && !B_KC, ktail = KTAILS && p.base.K % BK != 0;
     const int cus = compute_unit_count();
     const int64_t tn = A_KC && B_KC ? p.total : ceil_div(p.base.N, BN);
     const int pieces = cat_k ? p.slices * (p.each ? p.n : 1) : 1;
@@ -536,7 +541,7 @@ static hipError_t launch_fast_t(const GemmBf16Group& p0, hipStream_t st) {
     const int tiles = (int)(tm * tn) * pieces;
     if constexpr (A_KC) {
         if (mi < 4) {
-            if constexpr (B_KC) {
+            if constexpr (KTAILS) {
                 if (ktail) {
                     if (mi == 1) launch_tiles<A_KC, B_KC, EPI, 1, true>(p, tiles, cus, st);
                     else if (mi == 2) launch_tiles<A_KC, B_KC, EPI, 2, true>(p, tiles, cus, st);
@@ -550,7 +555,7 @@ static hipError_t launch_fast_t(const GemmBf16Group& p0, hipStream_t st) {
             return hipGetLastError();
         }
     }
-    if constexpr (A_KC && B_KC) {
+    if constexpr (KTAILS) {
         if (ktail) {      // (not traced)
             launch_tiles<A_KC, B_KC, EPI, 4, true>(p, tiles, cus, st);
             return hipGetLastError();
@@ -562,9 +567,9 @@ static hipError_t launch_fast_t(const GemmBf16Group& p0, hipStream_t st) {
             p.base.trace = tb;
             p.base.trace_cap = per_wg;
             if (tiles > cus)
-                hipLaunchKernelGGL((gemm_bf16_fast_kernel<A_KC, B_KC, EPI, true, true, false>), dim3(grid), dim3(NT), 0, st, p);
+                hipLaunchKernelGGL((gemm_bf16_fast_kernel<A_KC, B_KC, EPI, true, true, false, 4, Group>), dim3(grid), dim3(NT), 0, st, p);
             else
-                hipLaunchKernelGGL((gemm_bf16_fast_kernel<A_KC, B_KC, EPI, false, true, false>), dim3(grid), dim3(NT), 0, st, p);
+                hipLaunchKernelGGL((gemm_bf16_fast_kernel<A_KC, B_KC, EPI, false, true, false, 4, Group>), dim3(grid), dim3(NT), 0, st, p);
             return hipGetLastError();
         }
     }

@@ -45,7 +45,8 @@ enum class Epi : int {
     FwdStats = 0,   // per-row partial max / sum-exp / target logit (+ optional bf16 store of Y)
     DLogits = 1,    // D = (exp(Y - m)/sum - onehot) * scale, stored as bf16
     StoreF32 = 2,   // C = acc
-    AccumF32 = 3    // C += acc
+    AccumF32 = 3,   // C += acc
+    LogitsI8 = 4    // FwdStats of products of 8-bit integers with their scales (GemmI8Group)
 };
 
 struct GemmBf16Params {
@@ -269,24 +270,12 @@ constexpr int64_t I8_MAX_ROW = ((int64_t)1 << 17) - 128;
 static inline int64_t i8_row_stride(int64_t h) { return (h + 127) / 128 * 128; }
 hipError_t launch_quantize_rows(const void* x, int64_t N, int64_t h, vp_dtype dt, int8_t* q, float* scales, hipStream_t st);
 
-// The logits product of 8-bit integers over up to GEMM_GROUP_MAX shards, with its statistics (partials as in GemmBf16Params).
-struct GemmI8Shard {
-    const int8_t* W;
-    const float* scales;
-    void* out;           // [N, rows], or nullptr
-    int64_t offset;
-    int rows;
-};
-struct GemmI8Group {
-    const int8_t* H;
-    const float* scales;
-    const int64_t* labels;
-    int N, k;
-    int out_f32;         // type of the logits that are kept
-    float *part_max, *part_sum, *part_tgt;
-    int n, total;                  // shards; tile columns of all of them
-    int first[GEMM_GROUP_MAX];     // first tile column of shard r (INT_MAX from n on)
-    GemmI8Shard sh[GEMM_GROUP_MAX];
+// The logits product of 8-bit integers over up to GEMM_GROUP_MAX shards, with its statistics: that of the fast bf16 kernel, to
+// which two integers are one element (so K, lda and ldb are half of the integers' number, which is a multiple of 128).
+struct GemmI8Group : GemmBf16Group {
+    const float* row_scales;                     // [M]
+    const float* col_scales[GEMM_GROUP_MAX];     // [rows]
+    int out_f32;                                 // type of the logits that are kept: out of the shards is of this type
 };
 hipError_t launch_gemm_i8(const GemmI8Group& g, hipStream_t st);
 
