@@ -427,7 +427,8 @@ vp_status vp_output_fwd_i8_group(const int8_t* H, const float* H_scales, const i
  *   accepted [sequences] : out, int32, accepted drafts.  tokens [N] : out, int64: in a sequence's rows its accepted drafts, the
  *   next token, and -1 behind it.  Rows of no sequence are left as they were.  No output shares memory with an input or another
  *   output.
- * The workspace has vp_verify_workspace_bytes(sequences, V) bytes, V = the sum of rows ((size_t)-1 for invalid arguments).
+ * sequences <= 2^23.  The workspace has vp_verify_workspace_bytes(sequences, V) bytes, V = the sum of rows ((size_t)-1 for invalid
+ * arguments).
  */
 size_t vp_verify_workspace_bytes(int32_t sequences, int64_t V);
 vp_status vp_verify_drafts(const void* const* logits, const int64_t* rows, const int64_t* shard_offsets, int32_t p, vp_dtype dt,

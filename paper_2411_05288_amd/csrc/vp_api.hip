@@ -1177,8 +1177,10 @@ vp_status vp_output_fwd_i8(const int8_t* H, const float* H_scales, const int8_t*
 
 // ---- verification of drafts
 
+constexpr int32_t MAX_SEQUENCES = 1 << 23;      // a workgroup each at least: a launch has fewer than 2^32 threads
+
 size_t vp_verify_workspace_bytes(int32_t sequences, int64_t V) {
-    return sequences < 1 || V < 1 || V >= MAX_ELEMS ? (size_t)-1 : verify_workspace(sequences, V);
+    return sequences < 1 || sequences > MAX_SEQUENCES || V < 1 || V >= MAX_ELEMS ? (size_t)-1 : verify_workspace(sequences, V);
 }
 
 vp_status vp_verify_drafts(const void* const* logits, const int64_t* rows, const int64_t* shard_offsets, int32_t p, vp_dtype dt,
@@ -1195,7 +1197,7 @@ vp_status vp_verify_drafts(const void* const* logits, const int64_t* rows, const
          (uintptr_t)accepted) & 3u)
         return VP_ERR_INVALID_ARG;
     if ((((uintptr_t)drafts | (uintptr_t)starts | (uintptr_t)tokens) & 7u) || !aligned16(workspace)) return VP_ERR_INVALID_ARG;
-    if (p > VERIFY_MAX_SHARDS || N >= MAX_ELEMS) return VP_ERR_UNSUPPORTED;
+    if (p > VERIFY_MAX_SHARDS || N >= MAX_ELEMS || sequences > MAX_SEQUENCES) return VP_ERR_UNSUPPORTED;
     int64_t V = 0;
     for (int32_t r = 0; r < p; ++r) {
         if (!logits[r] || ((uintptr_t)logits[r] & (elem_bytes(dt) - 1)) || rows[r] < 1 || shard_offsets[r] < 0 || shard_offsets[r] > INT64_MAX - rows[r])

@@ -1,7 +1,8 @@
 // Verification of drafted tokens over the shards' logits and the draw of the next token (vp.h has the formulas).
 //
-// Two launches: the sums of the weights of every chunk of the row that the next token is drawn from, then the search for the
-// chunk and the token in it.  Every workgroup finds out by itself which row that is: a draft takes one logit of each model.
+// Two launches: the sums of the weights of every segment of 512 tokens of the row that the next token is drawn from, then the
+// search for the segment and the token in it.  Which row that is, every wavefront of the first launch finds out by itself: a draft
+// takes one logit of each model.
 // Probabilities and sums are in fp64: with 256000 tokens of like probability, an error of 1e-7 of the running sum would change
 // one draw in 40.
 #include "vp_internal.h"
@@ -10,24 +11,87 @@ namespace vp {
 
 namespace {
 
-constexpr int CHUNK = 4096, THREADS = 256, EACH = CHUNK / THREADS;
+constexpr int E = 8, SEGMENT = 64 * E, THREADS = 256, WAVES = THREADS / 64;
+constexpr int FILL = 8192;      // wavefronts that the chip holds at a time
+
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef unsigned short u16x8u __attribute__((ext_vector_type(8), aligned(2)));
 
 __device__ __forceinline__ float ld(const float* p) { return *p; }
 __device__ __forceinline__ float ld(const u16* p) { return __uint_as_float((unsigned)*p << 16); }
+// Eight logits from column j on, -inf past the end of the row (vectors start at any element).
+__device__ __forceinline__ void load8(float (&y)[E], const float* row, int j, int n) {
+    if (j + E <= n) {
+        const f32x4u a = *reinterpret_cast<const f32x4u*>(row + j), b = *reinterpret_cast<const f32x4u*>(row + j + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { y[e] = a[e]; y[e + 4] = b[e]; }
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] = j + e < n ? row[j + e] : -INFINITY;
+    }
+}
+__device__ __forceinline__ void load8(float (&y)[E], const u16* row, int j, int n) {
+    if (j + E <= n) {
+        const u16x8u a = *reinterpret_cast<const u16x8u*>(row + j);
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] = __uint_as_float((unsigned)a[e] << 16);
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] = j + e < n ? ld(row + j + e) : -INFINITY;
+    }
+}
 
-// The row of the next token, of a sequence that has rows.
-struct Row {
-    int64_t first, last, at;
-    double m, f, mz, fz;      // p = exp(Y - m) f, q = exp(Z - mz) fz
-    bool rejected;
+// exp(x) = 2^(n / 128) exp(r), n the integer nearest to 128 x / ln 2: a table of 2^(i / 128), i = 0 .. 127, and four terms of
+// the series of exp(r) - 1, |r| <= ln 2 / 256 (the fifth is below 2e-15).  The library's function takes twice the instructions.
+constexpr int TABLE = 128;
+__device__ __forceinline__ void fill_table(double* table) {
+    if (threadIdx.x < TABLE) table[threadIdx.x] = exp2((double)threadIdx.x / TABLE);
+    __syncthreads();
+}
+// Logits are held within what exp makes 0 or infinity of (a NaN stays one).
+struct Exp {
+    float low, high;
+    double m, f;      // f exp(y - m)
+    __device__ Exp(float m, double f) : low(m - 800.f), high(m + 800.f), m(m), f(f) {}
+    __device__ __forceinline__ double operator()(float y, const double* table) const {
+        y = y < low ? low : y;
+        y = y > high ? high : y;
+        const double x = (double)y - m;
+        constexpr double MAGIC = 6755399441055744.0;      // 1.5 2^52: a sum with it ends in the nearest integer
+        const double t = fma(x, TABLE / 0.693147180559945309417, MAGIC), n = t - MAGIC;
+        const double r = fma(n, -0.693147180559945309417 / TABLE, x);
+        double p = fma(r, 1.0 / 24, 1.0 / 6);
+        p = fma(p, r, 0.5);
+        p = fma(p, r, 1.0);
+        p *= r;
+        const int k = __double2loint(t);
+        const double a = table[k & (TABLE - 1)];
+        return ldexp(fma(a, p, a), k >> 7) * f;
+    }
 };
 
-// Where a token's logits of row i lie: the shard and the element, or -1.
+// A sequence's rows, and the row of the next token.
+struct Rows {
+    int64_t first, last;
+    __device__ Rows(const Verify& v, int b) {
+        first = bounded(v.starts[b], v.N);
+        last = bounded(v.starts[b + 1], v.N) - 1;
+    }
+    __device__ static int64_t bounded(int64_t s, int64_t N) { return s < 0 ? 0 : s > N ? N : s; }
+    __device__ bool any() const { return last >= first; }
+};
+// What the first launch leaves for the second.
+struct Found {
+    int64_t at;
+    float m, s, mz, sz;
+};
+
+// Where a token's logit of row i lies: the shard and the element, or shard -1.
 struct Place {
     int shard;
     size_t at;
 };
-__device__ Place place_of(const Verify& v, int64_t i, int64_t token) {
+__device__ __forceinline__ Place place_of(const Verify& v, int64_t i, int64_t token) {
     Place p{-1, 0};
     for (int r = 0; r < v.p; ++r) {
         const int64_t j = token - v.sh[r].offset;
@@ -36,205 +100,282 @@ __device__ Place place_of(const Verify& v, int64_t i, int64_t token) {
     return p;
 }
 
-// Whether sequence b has rows; its row of the next token.
+// Row of the first draft that is rejected, or the last row.
 template <typename T>
-__device__ bool find_row(const Verify& v, int b, Row& r) {
-    auto bounded = [&](int64_t s) { return s < 0 ? 0 : s > v.N ? v.N : s; };
-    r.first = bounded(v.starts[b]);
-    r.last = bounded(v.starts[b + 1]) - 1;
-    if (r.last < r.first) return false;
-    r.at = r.last;
-    r.rejected = false;
-    for (int64_t i0 = r.first; i0 < r.last; i0 += 64) {
+__device__ int64_t first_rejected(const Verify& v, const Rows& rows) {
+    for (int64_t i0 = rows.first; i0 < rows.last; i0 += 64) {
         const int64_t i = i0 + (threadIdx.x & 63);
         bool ok = true;
-        if (i < r.last) {
+        if (i < rows.last) {
+            const double m = v.gmax[i], s = v.gsum[i], u = v.uniforms[i];
+            const double mz = v.zmax ? v.zmax[i] : 0.f, sz = v.zmax ? v.zsum[i] : 0.f;
             const Place at = place_of(v, i, v.drafts[i]);
             double p = 0.0, q = 1.0;
             if (at.shard >= 0) {
-                p = exp((double)ld((const T*)v.sh[at.shard].Y + at.at) - v.gmax[i]) / v.gsum[i];
-                if (v.zmax) q = exp((double)ld((const T*)v.sh[at.shard].Z + at.at) - v.zmax[i]) / v.zsum[i];
+                p = exp((double)ld((const T*)v.sh[at.shard].Y + at.at) - m) / s;
+                if (v.zmax) q = exp((double)ld((const T*)v.sh[at.shard].Z + at.at) - mz) / sz;
             }
-            ok = (double)v.uniforms[i] * q < p;
+            ok = u * q < p;
         }
         const unsigned long long no = __ballot(!ok);
-        if (no) {
-            r.at = i0 + __builtin_ctzll(no);
-            r.rejected = true;
-            break;
+        if (no) return i0 + __builtin_ctzll(no);
+    }
+    return rows.last;
+}
+
+// Weights of the row of the next token.
+template <typename T>
+struct Weights {
+    const Verify& v;
+    const double* table;
+    int64_t at, skip;      // skip: a token of weight 0
+    bool model;
+    Exp p, q;
+    __device__ Weights(const Verify& v, const Found& f, bool rejected, const double* table)
+        : v(v), table(table), at(f.at), skip(rejected && !v.zmax ? v.drafts[f.at] : -1), model(rejected && v.zmax), p(f.m, 1.0 / f.s),
+          q(f.mz, 1.0 / f.sz) {}
+    // Eight of shard s from column j on.
+    __device__ __forceinline__ void load(double (&w)[E], const VerifyShard& s, int j) const {
+        const size_t row = (size_t)at * s.rows;
+        float y[E], z[E];
+        load8(y, (const T*)s.Y + row, j, s.rows);
+        if (model) load8(z, (const T*)s.Z + row, j, s.rows);
+#pragma unroll
+        for (int e = 0; e < E; ++e) w[e] = p(y[e], table);
+        if (model) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                w[e] -= q(z[e], table);
+                w[e] = w[e] < 0.0 ? 0.0 : w[e];      // (a NaN stays one)
+            }
+        }
+        const int64_t k = skip - s.offset - j;
+        if (skip >= 0 && k >= 0 && k < E) {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (k == e) w[e] = 0.0;
         }
     }
-    r.m = v.gmax[r.at];
-    r.f = 1.0 / v.gsum[r.at];
-    r.mz = r.fz = 0.0;
-    if (r.rejected && v.zmax) {
-        r.mz = v.zmax[r.at];
-        r.fz = 1.0 / v.zsum[r.at];
+    __device__ __forceinline__ double sum(const double (&w)[E]) const {
+        return ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
     }
-    return true;
-}
+};
 
-// Weight of column j of a shard; PLAIN: p alone.
-template <typename T, bool PLAIN>
-__device__ double weight(const Verify& v, const Row& r, const VerifyShard& s, int j) {
-    const size_t at = (size_t)r.at * s.rows + j;
-    double w = exp((double)ld((const T*)s.Y + at) - r.m) * r.f;
-    if (PLAIN || !r.rejected) return w;
-    if (v.zmax) w -= exp((double)ld((const T*)s.Z + at) - r.mz) * r.fz;
-    else if (v.drafts[r.at] == s.offset + j) w = 0.0;
-    return w < 0.0 ? 0.0 : w;      // (a NaN stays one)
-}
-
-__device__ __forceinline__ int shard_of(const Verify& v, int chunk) {
+__device__ __forceinline__ int shard_of(const Verify& v, int segment) {
     int r = 0;
-    while (r + 1 < v.p && chunk >= v.sh[r + 1].first) ++r;
+    for (int i = 1; i < v.p; ++i) r += segment >= v.sh[i].first;
     return r;
 }
 
-// Sum over the workgroup, in a fixed tree, in all threads; before: the sum over the threads before this one.
-__device__ double block_scan(double x, double& before, double* sh) {
-    double s = x;
+__device__ __forceinline__ double wave_sum(double x) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+    return x;
+}
+// Sum over the lanes up to this one.
+__device__ __forceinline__ double wave_scan(double x) {
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const double t = __shfl_up(s, o, 64);
-        if ((int)(threadIdx.x & 63) >= o) s += t;
+        const double t = __shfl_up(x, o, 64);
+        if ((int)(threadIdx.x & 63) >= o) x += t;
     }
-    __syncthreads();
-    if ((threadIdx.x & 63) == 63) sh[threadIdx.x >> 6] = s;
-    __syncthreads();
-    double base = 0.0;
-    for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) base += sh[w];
-    before = base + s - x;
-    return ((sh[0] + sh[1]) + sh[2]) + sh[3];
+    return x;
 }
 
-// A thread's part of a chunk: EACH consecutive columns.
-template <typename T, bool PLAIN>
-__device__ double thread_sum(const Verify& v, const Row& r, const VerifyShard& s, int chunk) {
-    const int j0 = (chunk - s.first) * CHUNK + threadIdx.x * EACH;
-    double sum = 0.0;
-    for (int j = j0; j < j0 + EACH && j < s.rows; ++j) sum += weight<T, PLAIN>(v, r, s, j);
-    return sum;
-}
-
+// Sequence b has the workgroups b * groups .. + groups - 1, whose wavefronts take its segments in turn.
 template <typename T>
-__global__ __launch_bounds__(THREADS) void verify_sums_kernel(Verify v, int chunks, double* part) {
-    __shared__ double sh[4];
-    Row r;
-    if (!find_row<T>(v, blockIdx.y, r)) return;
-    double before;
-    const double sum = block_scan(thread_sum<T, false>(v, r, v.sh[shard_of(v, blockIdx.x)], blockIdx.x), before, sh);
-    if (threadIdx.x == 0) part[(size_t)blockIdx.y * chunks + blockIdx.x] = sum;
+__global__ __launch_bounds__(THREADS) void verify_sums_kernel(Verify v, int segments, int groups, double* part, Found* found) {
+    __shared__ double table[TABLE];
+    const int b = blockIdx.x / groups, wave = (blockIdx.x % groups) * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Rows rows(v, b);
+    fill_table(table);
+    if (!rows.any()) return;
+    Found f{first_rejected<T>(v, rows), 0.f, 1.f, 0.f, 1.f};
+    const bool rejected = f.at < rows.last;
+    f.m = v.gmax[f.at];
+    f.s = v.gsum[f.at];
+    if (rejected && v.zmax) {
+        f.mz = v.zmax[f.at];
+        f.sz = v.zsum[f.at];
+    }
+    if (wave == 0 && (threadIdx.x & 63) == 0) found[b] = f;
+    const Weights<T> weights(v, f, rejected, table);
+    for (int g = wave; g < segments; g += groups * WAVES) {
+        const VerifyShard& s = v.sh[shard_of(v, g)];
+        double w[E];
+        weights.load(w, s, (g - s.first) * SEGMENT + (threadIdx.x & 63) * E);
+        const double sum = wave_sum(weights.sum(w));
+        if ((threadIdx.x & 63) == 0) part[(size_t)b * segments + g] = sum;
+    }
 }
 
-// Smallest value over the workgroup.
-__device__ int block_min(int x, int* sh) {
+// Of places in order, one to a lane (x its weight, upto the sum of them up to it): the first at which `upto` exceeds the target, or
+// where rounding leaves none the last one that has a weight; -1 if none has.
+__device__ __forceinline__ int choose(double x, double upto, double target) {
+    const unsigned long long some = __ballot(x > 0.0), hit = __ballot(x > 0.0 && upto > target);
+    return hit ? __builtin_ctzll(hit) : some ? 63 - __builtin_clzll(some) : -1;
+}
+
+// The token of a segment (for a whole wavefront): target is the share of its sum, not yet the sums before.
+template <typename T>
+__device__ int64_t token_of(const Verify& v, const Weights<T>& weights, int segment, double target) {
+    const VerifyShard& s = v.sh[shard_of(v, segment)];
+    const int j = (segment - s.first) * SEGMENT + (threadIdx.x & 63) * E;
+    double w[E];
+    weights.load(w, s, j);
+    const double mine = weights.sum(w), upto = wave_scan(mine);
+    const int l = choose(mine, upto, target);
+    int token = -1;
+    double run = upto - mine;
+    bool done = false;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) x = min(x, __shfl_xor(x, o, 64));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
-    __syncthreads();
-    return min(min(sh[0], sh[1]), min(sh[2], sh[3]));
+    for (int e = 0; e < E; ++e) {
+        run += w[e];
+        if (w[e] > 0.0 && !done) {
+            token = j + e;
+            done = run > target;
+        }
+    }
+    return s.offset + __shfl(token, l, 64);
 }
 
-// The first of n places, in order, at which the running sum exceeds `share` of the whole; or the last of positive weight, where
-// rounding leaves none.  sums(i): weights of the places, the same each time.  -1: no place of positive weight, or a sum that is
-// no number.
-template <typename F>
-__device__ int64_t pick(F sums, int n, double target, double& base, double* sh, int* shi) {
-    int last = -1;
-    double run = base;
-    for (int i0 = 0; i0 < n; i0 += THREADS) {
-        const int i = i0 + threadIdx.x;
-        const double x = i < n ? sums(i) : 0.0;
-        double before;
-        const double all = block_scan(x, before, sh);
-        const bool hit = x > 0.0 && run + before + x > target;
-        const int found = block_min(hit ? (int)threadIdx.x : THREADS, shi);
-        const int most = -block_min(x > 0.0 ? -(int)threadIdx.x - 1 : 0, shi) - 1;
-        if (found < THREADS) {
-            __syncthreads();
-            if ((int)threadIdx.x == found) sh[0] = run + before;
-            __syncthreads();
-            base = sh[0];
-            return i0 + found;
+// The draw from p itself, where nothing is left of the difference: every wavefront walks a quarter of the row, then one of them
+// its quarter again.
+template <typename T>
+__device__ int64_t plain_token(const Verify& v, const Found& f, double u, int segments, const double* table, double* sh) {
+    const Weights<T> weights(v, f, false, table);
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    auto from = [&](int w) { return (int)((int64_t)segments * w / WAVES); };
+    auto sum_of = [&](int g) {
+        const VerifyShard& s = v.sh[shard_of(v, g)];
+        double w[E];
+        weights.load(w, s, (g - s.first) * SEGMENT + lane * E);
+        return wave_sum(weights.sum(w));
+    };
+    double mine = 0.0;
+    for (int g = from(wave); g < from(wave + 1); ++g) mine += sum_of(g);
+    __syncthreads();
+    if (lane == 0) sh[wave] = mine;
+    __syncthreads();
+    double total = 0.0, base = 0.0;
+    for (int w = 0; w < WAVES; ++w) total += sh[w];
+    if (!(total > 0.0) || !(total < INFINITY)) return -1;
+    const double target = u * total;
+    int w = 0, chosen = -1;
+    for (double run = 0.0; w < WAVES; ++w) {
+        if (sh[w] > 0.0) {
+            chosen = w;
+            base = run;
+            if (run + sh[w] > target) break;
         }
-        if (most >= 0) {
-            last = i0 + most;
-            __syncthreads();
-            if ((int)threadIdx.x == most) sh[0] = run + before;
-            __syncthreads();
-            base = sh[0];
-            __syncthreads();
-        }
-        run += all;
+        run += sh[w];
     }
-    return last;
-}
-
-template <typename T, bool PLAIN>
-__device__ int64_t draw(const Verify& v, const Row& r, int chunks, double* part, double* sh, int* shi) {
-    double total = 0.0, before;
-    if (PLAIN) {
-        for (int c = 0; c < chunks; ++c) {
-            const double s = block_scan(thread_sum<T, true>(v, r, v.sh[shard_of(v, c)], c), before, sh);
-            if (threadIdx.x == 0) part[c] = s;
+    int segment = -1;
+    double before = 0.0;
+    for (int g = from(chosen); g < from(chosen + 1); ++g) {      // (all wavefronts walk the same quarter: the result is every thread's)
+        const double s = sum_of(g);
+        if (s > 0.0) {
+            segment = g;
+            before = base;
+            if (base + s > target) break;
         }
-        __syncthreads();
+        base += s;
     }
-    for (int c0 = 0; c0 < chunks; c0 += THREADS) total += block_scan(c0 + (int)threadIdx.x < chunks ? part[c0 + threadIdx.x] : 0.0, before, sh);
-    if (!(total < INFINITY)) return -1;
-    if (total == 0.0) return -2;
-    const double target = (double)v.uniforms[r.last] * total;
-    double base = 0.0;
-    const int c = (int)pick([&](int i) { return part[i]; }, chunks, target, base, sh, shi);
-    const VerifyShard& s = v.sh[shard_of(v, c)];
-    const int j0 = (c - s.first) * CHUNK, n = min(CHUNK, s.rows - j0);
-    const int64_t j = pick([&](int i) { return weight<T, PLAIN>(v, r, s, j0 + i); }, n, target, base, sh, shi);
-    return s.offset + j0 + j;
+    return token_of(v, weights, segment, target - before);
 }
 
 template <typename T>
-__global__ __launch_bounds__(THREADS) void verify_pick_kernel(Verify v, int chunks, double* part) {
-    __shared__ double sh[4];
-    __shared__ int shi[4];
-    const int b = blockIdx.x;
-    Row r;
-    if (!find_row<T>(v, b, r)) {
+__global__ __launch_bounds__(THREADS) void verify_pick_kernel(Verify v, int segments, const double* part, const Found* found) {
+    __shared__ double table[TABLE], sums[WAVES], chosen_base;
+    __shared__ int chosen_segment;
+    const int b = blockIdx.x, wave = threadIdx.x >> 6;
+    const Rows rows(v, b);
+    if (!rows.any()) {
         if (threadIdx.x == 0) v.accepted[b] = 0;
         return;
     }
-    part += (size_t)b * chunks;
-    int64_t token = draw<T, false>(v, r, chunks, part, sh, shi);
-    if (token == -2) token = r.rejected ? draw<T, true>(v, r, chunks, part, sh, shi) : -1;
-    if (token < 0) token = -1;
-    if (threadIdx.x == 0) v.accepted[b] = (int32_t)(r.at - r.first);
-    for (int64_t i = r.first + threadIdx.x; i <= r.last; i += THREADS)
-        v.tokens[i] = i < r.at ? v.drafts[i] : i == r.at ? token : -1;
+    const Found f = found[b];
+    const double u = v.uniforms[rows.last];
+    // the segments, an equal number of neighbours to every thread
+    part += (size_t)b * segments;
+    const int each = (segments + THREADS - 1) / THREADS, g0 = threadIdx.x * each, g1 = min(segments, g0 + each);
+    double mine = 0.0;
+    for (int g = g0; g < g1; ++g) mine += part[g];
+    const double in_wave = wave_scan(mine);
+    if ((threadIdx.x & 63) == 63) sums[wave] = in_wave;
+    if (threadIdx.x == 0) chosen_segment = -1;
+    fill_table(table);
+    const double total = ((sums[0] + sums[1]) + sums[2]) + sums[3], target = u * total;
+    int64_t token = -1;
+    const bool rejected = f.at < rows.last;
+    if (total > 0.0 && total < INFINITY) {
+        // every wavefront knows all sums: the first one in which the target is reached, or the last one with a weight
+        double base = 0.0, run = 0.0;
+        int w = -1;
+        for (int k = 0; k < WAVES; ++k) {
+            if (sums[k] > 0.0 && !(w >= 0 && run > target)) {
+                w = k;
+                base = run;
+            }
+            run += sums[k];
+        }
+        if (wave == w) {
+            const int l = choose(mine, base + in_wave, target);
+            if ((int)(threadIdx.x & 63) == l) {
+                int segment = -1;
+                double before = 0.0, at = base + in_wave - mine;
+                for (int g = g0; g < g1; ++g) {
+                    const double s = part[g];
+                    if (s > 0.0) {
+                        segment = g;
+                        before = at;
+                        if (at + s > target) break;
+                    }
+                    at += s;
+                }
+                chosen_segment = segment;
+                chosen_base = before;
+            }
+        }
+        __syncthreads();
+        const Weights<T> weights(v, f, rejected, table);
+        token = token_of(v, weights, chosen_segment, target - chosen_base);
+    } else if (total == 0.0 && rejected) {
+        token = plain_token<T>(v, f, u, segments, table, sums);
+    }
+    if (threadIdx.x == 0) v.accepted[b] = (int32_t)(f.at - rows.first);
+    for (int64_t i = rows.first + threadIdx.x; i <= rows.last; i += THREADS)
+        v.tokens[i] = i < f.at ? v.drafts[i] : i == f.at ? token : -1;
 }
 
 }  // namespace
 
+// The segments' sums, and the rows found.
 size_t verify_workspace(int64_t sequences, int64_t V) {
-    return align_up((size_t)sequences * (V / CHUNK + VERIFY_MAX_SHARDS) * sizeof(double), 256);
+    return align_up((size_t)sequences * ((V / SEGMENT + VERIFY_MAX_SHARDS) * sizeof(double) + sizeof(Found)), 256);
+}
+
+template <typename T>
+static void launch_verify_t(const Verify& v, int segments, int groups, double* part, Found* found, hipStream_t st) {
+    hipLaunchKernelGGL(verify_sums_kernel<T>, dim3(v.sequences * groups), dim3(THREADS), 0, st, v, segments, groups, part, found);
+    hipLaunchKernelGGL(verify_pick_kernel<T>, dim3(v.sequences), dim3(THREADS), 0, st, v, segments, part, found);
 }
 
 hipError_t launch_verify(const Verify& v0, vp_dtype dt, void* workspace, hipStream_t st) {
     ProfScope prof(K_VERIFY, st);
     Verify v = v0;
-    int chunks = 0;
+    int segments = 0;
     for (int r = 0; r < v.p; ++r) {
-        v.sh[r].first = chunks;
-        chunks += (int)ceil_div(v.sh[r].rows, CHUNK);
+        v.sh[r].first = segments;
+        segments += (int)ceil_div(v.sh[r].rows, SEGMENT);
     }
-    double* part = (double*)workspace;
-    if (dt == VP_F32) {
-        hipLaunchKernelGGL(verify_sums_kernel<float>, dim3(chunks, v.sequences), dim3(THREADS), 0, st, v, chunks, part);
-        hipLaunchKernelGGL(verify_pick_kernel<float>, dim3(v.sequences), dim3(THREADS), 0, st, v, chunks, part);
-    } else {
-        hipLaunchKernelGGL(verify_sums_kernel<u16>, dim3(chunks, v.sequences), dim3(THREADS), 0, st, v, chunks, part);
-        hipLaunchKernelGGL(verify_pick_kernel<u16>, dim3(v.sequences), dim3(THREADS), 0, st, v, chunks, part);
-    }
+    Found* found = (Found*)workspace;
+    double* part = (double*)(found + v.sequences);
+    // a wavefront for every segment where there are few, else as many as fit
+    const int most = (int)ceil_div(segments, WAVES), some = (int)ceil_div(FILL / WAVES, v.sequences);
+    const int groups = most < some ? most : some;
+    if (dt == VP_F32) launch_verify_t<float>(v, segments, groups, part, found, st);
+    else launch_verify_t<u16>(v, segments, groups, part, found, st);
     return hipGetLastError();
 }
 

@@ -135,7 +135,8 @@ def test_verify_size_limits_and_workspace(lib):
     assert 0 < need < BAD
     assert verify(lib, wb=need - 1) == WORKSPACE and verify(lib, ws=None) == WORKSPACE
     assert verify(lib, **MODEL, wb=need - 1) == WORKSPACE
-    for wrong in ((0, 70), (-1, 70), (3, 0), (3, -1), (3, 1 << 31)):
+    assert verify(lib, sequences=(1 << 23) + 1, wb=1 << 45) == UNSUPPORTED
+    for wrong in ((0, 70), (-1, 70), (3, 0), (3, -1), (3, 1 << 31), ((1 << 23) + 1, 70)):
         assert size(*wrong) == BAD
     assert verify(lib, p=65, Y=[P[0]] * 65, rows=[1] * 65, offsets=list(range(65))) == UNSUPPORTED
     assert verify(lib, N=1 << 31) == UNSUPPORTED
