@@ -1086,7 +1086,7 @@ size_t vp_output_i8_workspace_bytes(int32_t p, int64_t N, const int64_t* rows) {
     for (int32_t r0 = 0; r0 < p; r0 += GEMM_GROUP_MAX) {
         const int n = p - r0 < GEMM_GROUP_MAX ? p - r0 : GEMM_GROUP_MAX;
         int64_t tiles = 0;
-        for (int k = 0; k < n; ++k) tiles += fwd_tiles(rows[r0 + k]);
+        for (int k = 0; k < n; ++k) tiles += ceil_div(rows[r0 + k], gemm_i8_columns(N));
         const size_t b = align_up((size_t)(2 * tiles + n) * N * sizeof(float), 256);
         need = b > need ? b : need;
     }
@@ -1151,13 +1151,12 @@ vp_status vp_output_fwd_i8_group(const int8_t* H, const float* H_scales, const i
             g.sh[i].ld = g.sh[i].rows = l.rows[i] = (int)rows[r];
             g.sh[i].offset = l.offset[i] = shard_offsets[r];
             g.col_scales[i] = W_scales[r];
-            l.first[i + 1] = l.first[i] + (int)fwd_tiles(rows[r]);
+            l.first[i + 1] = l.first[i] + (int)ceil_div(rows[r], gemm_i8_columns(N));
         }
-        gemm_bf16_group_finish(g, n);
-        float* pm = (float*)workspace;
-        g.base.part_max = pm;
-        g.base.part_sum = pm + (int64_t)g.total * N;
-        g.base.part_tgt = pm + 2 * (int64_t)g.total * N;
+        g.n = n;
+        g.base.part_max = (float*)workspace;
+        g.base.part_sum = g.base.part_max + (int64_t)l.first[n] * N;
+        g.base.part_tgt = g.base.part_max + 2 * (int64_t)l.first[n] * N;
         if (launch_gemm_i8(g, st) != hipSuccess ||
             launch_fold_partials(g.base.part_max, g.base.part_sum, g.base.part_tgt, l, (int)N, labels, local_max + r0 * N,
                                  local_sumexp + r0 * N, local_target + r0 * N, st) != hipSuccess)

@@ -1,12 +1,237 @@
-// The output layer's logits from 8-bit integers: the fast kernel (vp_gemm_bf16_fast.h) with integer products, whose operands of 16
-// bytes hold 16 integers in place of 8 numbers; data movement, tiles and tile order are the same.
+// The output layer's logits from 8-bit integers.  Many tokens: the fast kernel (vp_gemm_bf16_fast.h) with integer products, whose
+// operands of 16 bytes hold 16 integers in place of 8 numbers; data movement, tiles and tile order are the same.  Few tokens: a
+// kernel of its own, below, that is bound by reading W.
+#include <climits>
+
 #include "vp_gemm_bf16_fast.h"
 
 namespace vp {
 
-hipError_t launch_gemm_i8(const GemmI8Group& g, hipStream_t st) {
+namespace {
+
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef unsigned uintx4u __attribute__((ext_vector_type(4), aligned(2)));
+
+// Few tokens: 32 TI of them and 32 WAVES vocabulary rows in a workgroup of WAVES wavefronts, which take 32 rows each.  W is read
+// once, so what counts is that enough of it is on its way: a ring of SLOTS k tiles of 128 integers, all but one of them in flight,
+// and as many workgroups on a compute unit as the LDS holds, so that one loads while another is at its ends.  A load instruction
+// takes 8 whole lines of 128 bytes (past the caches: W is not read again), 16 bytes per lane, straight into LDS.
+//
+// A slot holds rows of 128 bytes, of W and then of H.  Chunk c of row r (16 bytes) sits at position c ^ (r / 2 % 8): 16
+// consecutive rows, which a read of LDS serves at a time, have the same chunk in 16 different groups of banks.
+constexpr int FEW_K = 128, FEW_SLOTS = 4;
+template <int TI, int WAVES>
+struct Few {
+    static constexpr int COLS = 32 * WAVES, ROWS = 32 * TI, SLOT = (COLS + ROWS) * FEW_K;
+    static constexpr int LOADS_W = COLS / 8 / WAVES, LOADS_H = (ROWS / 8 + WAVES - 1) / WAVES;
+    // outputs of 32 tokens are staged in a slot; rows padded by 16 bytes
+    static constexpr int STAGE_ROW = COLS * 4 + 16;
+    static_assert(32 * STAGE_ROW <= SLOT, "staging exceeds a slot");
+};
+
+template <int TI, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group gg) {
+    using F = Few<TI, WAVES>;
+    __shared__ __attribute__((aligned(1024))) char slot0[F::SLOT];
+    __shared__ __attribute__((aligned(1024))) char slot1[F::SLOT];
+    __shared__ __attribute__((aligned(1024))) char slot2[F::SLOT];
+    __shared__ __attribute__((aligned(1024))) char slot3[F::SLOT];
+    static_assert(FEW_SLOTS == 4, "slots");
+    const GemmBf16Params& g = gg.base;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l32 = lane & 31, hf = lane >> 5;
+    const int shard = shard_of(gg, blockIdx.x);
+    const GemmBf16Shard& s = gg.sh[shard];
+    const int tile = (int)blockIdx.x - gg.first[shard], n0 = tile * F::COLS, k = g.K * 2;
+    const unsigned w_bytes = (unsigned)s.rows * (unsigned)k, h_bytes = (unsigned)g.M * (unsigned)k;
+
+    // this lane's columns are cbase + 8 (r / 4) + r % 4
+    const int cbase = n0 + wave * 32 + 4 * hf;
+    const float* col_scales = gg.col_scales[shard];
+    float cs[16], rs[TI];
+    int64_t label[TI];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) cs[r] = col_scales[min(cbase + 8 * (r >> 2) + (r & 3), s.rows - 1)];
+#pragma unroll
+    for (int t = 0; t < TI; ++t) {
+        const int m = min(t * 32 + l32, g.M - 1);
+        rs[t] = gg.row_scales[m];
+        label[t] = g.labels[m];
+    }
+
+    unsigned w_off[F::LOADS_W], h_off[F::LOADS_H];
+#pragma unroll
+    for (int i = 0; i < F::LOADS_W; ++i) {
+        const int row = (wave * F::LOADS_W + i) * 8 + (lane >> 3), c = (lane & 7) ^ (row >> 1 & 7);
+        w_off[i] = (unsigned)(n0 + row) * (unsigned)k + (unsigned)c * 16u;
+    }
+#pragma unroll
+    for (int i = 0; i < F::LOADS_H; ++i) {
+        const int row = (wave * F::LOADS_H + i) * 8 + (lane >> 3), c = (lane & 7) ^ (row >> 1 & 7);
+        h_off[i] = (unsigned)row * (unsigned)k + (unsigned)c * 16u;
+    }
+    auto slot = [&](auto i) -> char* {
+        constexpr int S = decltype(i)::value % FEW_SLOTS;
+        if constexpr (S == 0) return slot0;
+        else if constexpr (S == 1) return slot1;
+        else if constexpr (S == 2) return slot2;
+        else return slot3;
+    };
+    // The k advance is applied to the descriptors: a k tile past the end has empty ones, no access is made and zeros arrive, as
+    // they do for rows past the end of W or H.  Every workgroup begins at another k tile (sums of integers have no order).
+    const int nkt = k / FEW_K, turn = (int)(blockIdx.x) % nkt;
+    auto load = [&](auto i, int kt) {
+        char* to = slot(i);
+        const int at = kt + turn < nkt ? kt + turn : kt + turn - nkt;
+        const unsigned adv = (unsigned)(at * FEW_K);
+        const unsigned wa = kt < nkt ? adv : w_bytes, ha = kt < nkt ? adv : h_bytes;
+        const __amdgpu_buffer_rsrc_t rw = __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)s.B + wa), 0, (int)(w_bytes - wa), 0x00020000);
+        const __amdgpu_buffer_rsrc_t rh = __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)g.A + ha), 0, (int)(h_bytes - ha), 0x00020000);
+#pragma unroll
+        for (int j = 0; j < F::LOADS_W; ++j)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (lds_ptr)(to + (wave * F::LOADS_W + j) * 1024), 16, (int)w_off[j], 0, 0, 2);
+#pragma unroll
+        for (int j = 0; j < F::LOADS_H; ++j)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rh, (lds_ptr)(to + F::COLS * FEW_K + (wave * F::LOADS_H + j) * 1024), 16, (int)h_off[j], 0, 0, 0);
+    };
+    int w_at[4], h_at[4];      // of the four 32-wide steps of a k tile
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+        const int pos = ((2 * kk + hf) ^ (l32 >> 1 & 7)) * 16;
+        w_at[kk] = (wave * 32 + l32) * FEW_K + pos;
+        h_at[kk] = F::COLS * FEW_K + l32 * FEW_K + pos;
+    }
+    intx16 acc[TI] = {};
+    auto multiply = [&](auto i) {
+        const char* from = slot(i);
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+            const intx4 w = *reinterpret_cast<const intx4*>(from + w_at[kk]);
+#pragma unroll
+            for (int t = 0; t < TI; ++t)
+                acc[t] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w, *reinterpret_cast<const intx4*>(from + h_at[kk] + t * 32 * FEW_K), acc[t], 0, 0, 0);
+        }
+    };
+    // k tile kt: its loads are the oldest of three tiles'; behind the barrier all wavefronts' have landed, and the slot of the tile
+    // before is free.
+    constexpr int PER = F::LOADS_W + F::LOADS_H;
+    static_assert(2 * PER < 64, "memory counter");
+    auto step = [&](auto i, int kt) {
+        __builtin_amdgcn_s_waitcnt(((2 * PER) & 15) | (((2 * PER) >> 4) << 14) | 0x70);      // vmcnt(2 PER), lgkmcnt(0)
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        load(std::integral_constant<int, decltype(i)::value + 3>{}, kt + 3);
+        multiply(i);
+    };
+    constexpr std::integral_constant<int, 0> I0;
+    constexpr std::integral_constant<int, 1> I1;
+    constexpr std::integral_constant<int, 2> I2;
+    constexpr std::integral_constant<int, 3> I3;
+    load(I0, 0);
+    load(I1, 1);
+    load(I2, 2);
+    int kt = 0;
+    for (int it = nkt / 4; it > 0; --it, kt += 4) {
+        step(I0, kt);
+        step(I1, kt + 1);
+        step(I2, kt + 2);
+        step(I3, kt + 3);
+    }
+    if (kt < nkt) {
+        step(I0, kt);
+        if (kt + 1 < nkt) {
+            step(I1, kt + 1);
+            if (kt + 2 < nkt) step(I2, kt + 2);
+        }
+    }
+    __syncthreads();      // no load is in flight, and no wavefront reads a slot
+    // the statistics of the wavefronts' columns; outputs are staged in slot 0
+    float(*xm)[F::ROWS] = reinterpret_cast<float(*)[F::ROWS]>(slot1), (*xs)[F::ROWS] = xm + WAVES;
+
+#pragma unroll
+    for (int t = 0; t < TI; ++t) {
+        if (t * 32 >= g.M) break;
+        const int m = t * 32 + l32;
+        float y[16], v = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            y[r] = cbase + 8 * (r >> 2) + (r & 3) < s.rows ? (float)acc[t][r] * cs[r] * rs[t] : -INFINITY;
+            v = fmaxf(v, y[r]);
+        }
+        v = fmaxf(v, __shfl_xor(v, 32, 64));
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum += exp2_fast((y[r] - v) * LOG2E);
+        sum += __shfl_xor(sum, 32, 64);
+        if (hf == 0) {
+            xm[wave][m] = v;
+            xs[wave][m] = sum;
+        }
+        const int64_t at = label[t] - s.offset - cbase;
+        if (label[t] >= 0 && at >= 0 && at < 32 && (at & 4) == 0 && at + cbase < s.rows && m < g.M) {
+            float target = 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (at == 8 * (r >> 2) + (r & 3)) target = y[r];
+            g.part_tgt[(size_t)shard * g.M + m] = target;
+        }
+        if (s.out) {
+            if (t) __syncthreads();
+            const int cols = min(F::COLS, s.rows - n0), rows = min(32, g.M - t * 32);
+            const int elem = gg.out_f32 ? 4 : 2, per_row = F::COLS * elem / 16;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                char* to = slot0 + l32 * F::STAGE_ROW + (wave * 32 + 8 * q + 4 * hf) * elem;
+                if (gg.out_f32) *reinterpret_cast<floatx4*>(to) = floatx4{y[4 * q], y[4 * q + 1], y[4 * q + 2], y[4 * q + 3]};
+                else *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(y[4 * q], y[4 * q + 1]), pack_bf16x2(y[4 * q + 2], y[4 * q + 3]));
+            }
+            __syncthreads();
+            for (int i = threadIdx.x; i < rows * per_row; i += 64 * WAVES) {
+                const int row = i / per_row, c = i % per_row * (16 / elem);
+                const char* from = slot0 + row * F::STAGE_ROW + c * elem;
+                char* to = (char*)s.out + ((size_t)(t * 32 + row) * s.ld + n0 + c) * elem;
+                if (c + 16 / elem <= cols) *reinterpret_cast<uintx4u*>(to) = *reinterpret_cast<const uintx4*>(from);
+                else
+                    for (int e = 0; c + e < cols; ++e) {
+                        if (gg.out_f32) ((float*)to)[e] = ((const float*)from)[e];
+                        else ((u16*)to)[e] = ((const u16*)from)[e];
+                    }
+            }
+        }
+    }
+    __syncthreads();
+    for (int m = threadIdx.x; m < F::ROWS && m < g.M; m += 64 * WAVES) {
+        float v = xm[0][m], sum = 0.f;
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v = fmaxf(v, xm[w][m]);
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w)
+            if (xm[w][m] > -INFINITY) sum += xs[w][m] * __expf(xm[w][m] - v);
+        g.part_max[(size_t)blockIdx.x * g.M + m] = v;
+        g.part_sum[(size_t)blockIdx.x * g.M + m] = sum;
+    }
+}
+
+}  // namespace
+
+// Columns of a tile: a row of partial statistics each.
+int gemm_i8_columns(int64_t N) { return N <= 64 ? 128 : BN; }
+
+hipError_t launch_gemm_i8(const GemmI8Group& g0, hipStream_t st) {
     ProfScope prof(K_GEMM_I8, st);
-    return launch_fast_t<true, true, Epi::LogitsI8>(g, st);
+    GemmI8Group g = g0;
+    const int cols = gemm_i8_columns(g.base.M);
+    g.total = 0;
+    for (int r = 0; r < GEMM_GROUP_MAX; ++r) {
+        g.first[r] = r < g.n ? g.total : INT_MAX;
+        if (r < g.n) g.total += (int)ceil_div(g.sh[r].rows, cols);
+    }
+    g.slices = 1;
+    if (g.base.M > 64) return launch_fast_t<true, true, Epi::LogitsI8>(g, st);
+    if (g.base.M <= 32) hipLaunchKernelGGL((gemm_i8_few_kernel<1, 4>), dim3(g.total), dim3(256), 0, st, g);
+    else hipLaunchKernelGGL((gemm_i8_few_kernel<2, 4>), dim3(g.total), dim3(256), 0, st, g);
+    return hipGetLastError();
 }
 
 }  // namespace vp

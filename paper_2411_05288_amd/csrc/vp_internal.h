@@ -277,6 +277,8 @@ struct GemmI8Group : GemmBf16Group {
     const float* col_scales[GEMM_GROUP_MAX];     // [rows]
     int out_f32;                                 // type of the logits that are kept: out of the shards is of this type
 };
+// Columns of a tile of N tokens: a row of partial statistics each (the launch fills first and total).
+int gemm_i8_columns(int64_t N);
 hipError_t launch_gemm_i8(const GemmI8Group& g, hipStream_t st);
 
 // Verification of drafts: see vp.h.
