@@ -5,6 +5,8 @@
 // takes one logit of each model.
 // Probabilities and sums are in fp64: with 256000 tokens of like probability, an error of 1e-7 of the running sum would change
 // one draw in 40.
+#include <climits>
+
 #include "vp_internal.h"
 
 namespace vp {
@@ -19,25 +21,34 @@ typedef unsigned short u16x8u __attribute__((ext_vector_type(8), aligned(2)));
 
 __device__ __forceinline__ float ld(const float* p) { return *p; }
 __device__ __forceinline__ float ld(const u16* p) { return __uint_as_float((unsigned)*p << 16); }
-// Eight logits from column j on, -inf past the end of the row (vectors start at any element).
-__device__ __forceinline__ void load8(float (&y)[E], const float* row, int j, int n) {
-    if (j + E <= n) {
-        const f32x4u a = *reinterpret_cast<const f32x4u*>(row + j), b = *reinterpret_cast<const f32x4u*>(row + j + 4);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) { y[e] = a[e]; y[e + 4] = b[e]; }
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) y[e] = j + e < n ? row[j + e] : -INFINITY;
+// Eight logits as they are stored (vectors start at any element).
+template <typename T>
+struct Raw;
+template <>
+struct Raw<float> {
+    f32x4u a, b;
+    __device__ __forceinline__ void load(const float* p) {
+        a = *reinterpret_cast<const f32x4u*>(p);
+        b = *reinterpret_cast<const f32x4u*>(p + 4);
     }
-}
-__device__ __forceinline__ void load8(float (&y)[E], const u16* row, int j, int n) {
+    __device__ __forceinline__ float operator[](int e) const { return e < 4 ? a[e] : b[e - 4]; }
+    __device__ __forceinline__ void set(int e, float f) { if (e < 4) a[e] = f; else b[e - 4] = f; }
+};
+template <>
+struct Raw<u16> {
+    u16x8u a;
+    __device__ __forceinline__ void load(const u16* p) { a = *reinterpret_cast<const u16x8u*>(p); }
+    __device__ __forceinline__ float operator[](int e) const { return __uint_as_float((unsigned)a[e] << 16); }
+    __device__ __forceinline__ void set(int e, float f) { a[e] = (u16)(__float_as_uint(f) >> 16); }
+};
+// Columns j .. j + 7 of a row of n, -inf past its end.
+template <typename T>
+__device__ __forceinline__ void load8(Raw<T>& y, const T* row, int j, int n) {
     if (j + E <= n) {
-        const u16x8u a = *reinterpret_cast<const u16x8u*>(row + j);
-#pragma unroll
-        for (int e = 0; e < E; ++e) y[e] = __uint_as_float((unsigned)a[e] << 16);
+        y.load(row + j);
     } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e) y[e] = j + e < n ? ld(row + j + e) : -INFINITY;
+        for (int e = 0; e < E; ++e) y.set(e, j + e < n ? ld(row + j + e) : -INFINITY);
     }
 }
 
@@ -48,15 +59,13 @@ __device__ __forceinline__ void fill_table(double* table) {
     if (threadIdx.x < TABLE) table[threadIdx.x] = exp2((double)threadIdx.x / TABLE);
     __syncthreads();
 }
-// Logits are held within what exp makes 0 or infinity of (a NaN stays one).
 struct Exp {
-    float low, high;
+    float low;
     double m, f;      // f exp(y - m)
-    __device__ Exp(float m, double f) : low(m - 800.f), high(m + 800.f), m(m), f(f) {}
+    // (exp(-800) is 0; y = -inf would leave no n)
+    __device__ Exp(float m, double f) : low(m - 800.f), m(m), f(f) {}
     __device__ __forceinline__ double operator()(float y, const double* table) const {
-        y = y < low ? low : y;
-        y = y > high ? high : y;
-        const double x = (double)y - m;
+        const double x = (double)__builtin_elementwise_maximum(y, low) - m;      // (a NaN stays one)
         constexpr double MAGIC = 6755399441055744.0;      // 1.5 2^52: a sum with it ends in the nearest integer
         const double t = fma(x, TABLE / 0.693147180559945309417, MAGIC), n = t - MAGIC;
         const double r = fma(n, -0.693147180559945309417 / TABLE, x);
@@ -68,6 +77,24 @@ struct Exp {
         const double a = table[k & (TABLE - 1)];
         return ldexp(fma(a, p, a), k >> 7) * f;
     }
+};
+
+// What a lane holds of the shard of its number: reading the arguments one shard after the other takes a memory latency each.
+struct Lanes {
+    int64_t offset;
+    int first, rows;
+    __device__ explicit Lanes(const Verify& v) {
+        const int l = threadIdx.x & 63;
+        offset = 0;
+        first = INT_MAX;
+        rows = 0;
+        if (l < v.p) {
+            offset = v.sh[l].offset;
+            first = v.sh[l].first;
+            rows = v.sh[l].rows;
+        }
+    }
+    __device__ __forceinline__ int shard_of(int segment) const { return __popcll(__ballot(segment >= first)) - 1; }
 };
 
 // A sequence's rows, and the row of the next token.
@@ -91,25 +118,28 @@ struct Place {
     int shard;
     size_t at;
 };
-__device__ __forceinline__ Place place_of(const Verify& v, int64_t i, int64_t token) {
-    Place p{-1, 0};
-    for (int r = 0; r < v.p; ++r) {
-        const int64_t j = token - v.sh[r].offset;
-        if (token >= v.sh[r].offset && j < v.sh[r].rows) p = {r, (size_t)i * v.sh[r].rows + (size_t)j};
+__device__ __forceinline__ Place place_of(const Lanes& shards, int p, int64_t i, int64_t token) {
+    Place at{-1, 0};
+    for (int r = 0; r < p; ++r) {
+        const int64_t first = (int64_t)(unsigned)__builtin_amdgcn_readlane((int)shards.offset, r) |
+                              (int64_t)__builtin_amdgcn_readlane((int)(shards.offset >> 32), r) << 32;
+        const int rows = __builtin_amdgcn_readlane(shards.rows, r);
+        const int64_t j = token - first;
+        if (token >= first && j < rows) at = {r, (size_t)i * rows + (size_t)j};
     }
-    return p;
+    return at;
 }
 
 // Row of the first draft that is rejected, or the last row.
 template <typename T>
-__device__ int64_t first_rejected(const Verify& v, const Rows& rows) {
+__device__ __forceinline__ int64_t first_rejected(const Verify& v, const Lanes& shards, const Rows& rows) {
     for (int64_t i0 = rows.first; i0 < rows.last; i0 += 64) {
         const int64_t i = i0 + (threadIdx.x & 63);
         bool ok = true;
         if (i < rows.last) {
             const double m = v.gmax[i], s = v.gsum[i], u = v.uniforms[i];
             const double mz = v.zmax ? v.zmax[i] : 0.f, sz = v.zmax ? v.zsum[i] : 0.f;
-            const Place at = place_of(v, i, v.drafts[i]);
+            const Place at = place_of(shards, v.p, i, v.drafts[i]);
             double p = 0.0, q = 1.0;
             if (at.shard >= 0) {
                 p = exp((double)ld((const T*)v.sh[at.shard].Y + at.at) - m) / s;
@@ -131,66 +161,76 @@ struct Weights {
     int64_t at, skip;      // skip: a token of weight 0
     bool model;
     Exp p, q;
+    Raw<T> y, z;           // eight logits of each model, of shard `shard` from column j on
+    int shard, j;
     __device__ Weights(const Verify& v, const Found& f, bool rejected, const double* table)
         : v(v), table(table), at(f.at), skip(rejected && !v.zmax ? v.drafts[f.at] : -1), model(rejected && v.zmax), p(f.m, 1.0 / f.s),
           q(f.mz, 1.0 / f.sz) {}
-    // Eight of shard s from column j on.
-    __device__ __forceinline__ void load(double (&w)[E], const VerifyShard& s, int j) const {
+    // This lane's eight of a segment.
+    __device__ __forceinline__ void load(const Lanes& shards, int segment) {
+        shard = shards.shard_of(segment);
+        const VerifyShard& s = v.sh[shard];
+        j = (segment - s.first) * SEGMENT + (threadIdx.x & 63) * E;
         const size_t row = (size_t)at * s.rows;
-        float y[E], z[E];
         load8(y, (const T*)s.Y + row, j, s.rows);
         if (model) load8(z, (const T*)s.Z + row, j, s.rows);
+    }
+    __device__ __forceinline__ void get(double (&w)[E]) const {
 #pragma unroll
         for (int e = 0; e < E; ++e) w[e] = p(y[e], table);
         if (model) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 w[e] -= q(z[e], table);
-                w[e] = w[e] < 0.0 ? 0.0 : w[e];      // (a NaN stays one)
+                w[e] = fmax(w[e], 0.0) + w[e] * 0.0;      // (the second term is NaN where the first would hide one)
             }
         }
-        const int64_t k = skip - s.offset - j;
+        const int64_t k = skip - v.sh[shard].offset - j;
         if (skip >= 0 && k >= 0 && k < E) {
 #pragma unroll
             for (int e = 0; e < E; ++e)
                 if (k == e) w[e] = 0.0;
         }
     }
-    __device__ __forceinline__ double sum(const double (&w)[E]) const {
+    __device__ __forceinline__ static double sum(const double (&w)[E]) {
         return ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+    }
+    __device__ __forceinline__ double sum() const {
+        double w[E];
+        get(w);
+        return sum(w);
     }
 };
 
-__device__ __forceinline__ int shard_of(const Verify& v, int segment) {
-    int r = 0;
-    for (int i = 1; i < v.p; ++i) r += segment >= v.sh[i].first;
-    return r;
+// Sum over the lanes up to this one (the last lane's: over all).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double add_moved(double x) {      // + 0 where no lane moves in
+    const int low = __builtin_amdgcn_update_dpp(0, __double2loint(x), CTRL, ROWS, 0xf, false);
+    const int high = __builtin_amdgcn_update_dpp(0, __double2hiint(x), CTRL, ROWS, 0xf, false);
+    return x + __hiloint2double(high, low);
 }
-
-__device__ __forceinline__ double wave_sum(double x) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
-    return x;
-}
-// Sum over the lanes up to this one.
 __device__ __forceinline__ double wave_scan(double x) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const double t = __shfl_up(x, o, 64);
-        if ((int)(threadIdx.x & 63) >= o) x += t;
-    }
-    return x;
+    x = add_moved<0x111, 0xf>(x);      // from 1, 2, 4, 8 lanes before, within 16
+    x = add_moved<0x112, 0xf>(x);
+    x = add_moved<0x114, 0xf>(x);
+    x = add_moved<0x118, 0xf>(x);
+    x = add_moved<0x142, 0xa>(x);      // the last lane of 16 into the next 16, of 32 into the next 32
+    return add_moved<0x143, 0xc>(x);
+}
+__device__ __forceinline__ double last_lane(double x) {
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(x), 63), __builtin_amdgcn_readlane(__double2loint(x), 63));
 }
 
 // Sequence b has the workgroups b * groups .. + groups - 1, whose wavefronts take its segments in turn.
 template <typename T>
-__global__ __launch_bounds__(THREADS) void verify_sums_kernel(Verify v, int segments, int groups, double* part, Found* found) {
+__global__ __launch_bounds__(THREADS, 8) void verify_sums_kernel(Verify v, int segments, int groups, double* part, Found* found) {
     __shared__ double table[TABLE];
     const int b = blockIdx.x / groups, wave = (blockIdx.x % groups) * WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Rows rows(v, b);
+    const Lanes shards(v);
     fill_table(table);
     if (!rows.any()) return;
-    Found f{first_rejected<T>(v, rows), 0.f, 1.f, 0.f, 1.f};
+    Found f{first_rejected<T>(v, shards, rows), 0.f, 1.f, 0.f, 1.f};
     const bool rejected = f.at < rows.last;
     f.m = v.gmax[f.at];
     f.s = v.gsum[f.at];
@@ -199,13 +239,11 @@ __global__ __launch_bounds__(THREADS) void verify_sums_kernel(Verify v, int segm
         f.sz = v.zsum[f.at];
     }
     if (wave == 0 && (threadIdx.x & 63) == 0) found[b] = f;
-    const Weights<T> weights(v, f, rejected, table);
+    Weights<T> w(v, f, rejected, table);
     for (int g = wave; g < segments; g += groups * WAVES) {
-        const VerifyShard& s = v.sh[shard_of(v, g)];
-        double w[E];
-        weights.load(w, s, (g - s.first) * SEGMENT + (threadIdx.x & 63) * E);
-        const double sum = wave_sum(weights.sum(w));
-        if ((threadIdx.x & 63) == 0) part[(size_t)b * segments + g] = sum;
+        w.load(shards, g);
+        const double sum = wave_scan(w.sum());
+        if ((threadIdx.x & 63) == 63) part[(size_t)b * segments + g] = sum;
     }
 }
 
@@ -218,11 +256,10 @@ __device__ __forceinline__ int choose(double x, double upto, double target) {
 
 // The token of a segment (for a whole wavefront): target is the share of its sum, not yet the sums before.
 template <typename T>
-__device__ int64_t token_of(const Verify& v, const Weights<T>& weights, int segment, double target) {
-    const VerifyShard& s = v.sh[shard_of(v, segment)];
-    const int j = (segment - s.first) * SEGMENT + (threadIdx.x & 63) * E;
+__device__ __forceinline__ int64_t token_of(Weights<T>& weights, const Lanes& shards, int segment, double target) {
+    weights.load(shards, segment);
     double w[E];
-    weights.load(w, s, j);
+    weights.get(w);
     const double mine = weights.sum(w), upto = wave_scan(mine);
     const int l = choose(mine, upto, target);
     int token = -1;
@@ -232,37 +269,37 @@ __device__ int64_t token_of(const Verify& v, const Weights<T>& weights, int segm
     for (int e = 0; e < E; ++e) {
         run += w[e];
         if (w[e] > 0.0 && !done) {
-            token = j + e;
+            token = weights.j + e;
             done = run > target;
         }
     }
-    return s.offset + __shfl(token, l, 64);
+    return weights.v.sh[weights.shard].offset + __shfl(token, l, 64);
 }
 
-// The draw from p itself, where nothing is left of the difference: every wavefront walks a quarter of the row, then one of them
-// its quarter again.
+// The draw from p itself, where nothing is left of the difference: every wavefront walks a quarter of the row, then all of them the
+// quarter in which the target is reached.
 template <typename T>
-__device__ int64_t plain_token(const Verify& v, const Found& f, double u, int segments, const double* table, double* sh) {
-    const Weights<T> weights(v, f, false, table);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+__device__ int64_t plain_token(const Verify& v, const Found& f, const Lanes& shards, double u, int segments, const double* table,
+                               double* sh) {
+    Weights<T> weights(v, f, false, table);
+    const int wave = threadIdx.x >> 6;
     auto from = [&](int w) { return (int)((int64_t)segments * w / WAVES); };
     auto sum_of = [&](int g) {
-        const VerifyShard& s = v.sh[shard_of(v, g)];
-        double w[E];
-        weights.load(w, s, (g - s.first) * SEGMENT + lane * E);
-        return wave_sum(weights.sum(w));
+        weights.load(shards, g);
+        return last_lane(wave_scan(weights.sum()));
     };
     double mine = 0.0;
     for (int g = from(wave); g < from(wave + 1); ++g) mine += sum_of(g);
     __syncthreads();
-    if (lane == 0) sh[wave] = mine;
+    if ((threadIdx.x & 63) == 0) sh[wave] = mine;
     __syncthreads();
     double total = 0.0, base = 0.0;
     for (int w = 0; w < WAVES; ++w) total += sh[w];
     if (!(total > 0.0) || !(total < INFINITY)) return -1;
     const double target = u * total;
-    int w = 0, chosen = -1;
-    for (double run = 0.0; w < WAVES; ++w) {
+    int chosen = -1;
+    double run = 0.0;
+    for (int w = 0; w < WAVES; ++w) {
         if (sh[w] > 0.0) {
             chosen = w;
             base = run;
@@ -272,7 +309,7 @@ __device__ int64_t plain_token(const Verify& v, const Found& f, double u, int se
     }
     int segment = -1;
     double before = 0.0;
-    for (int g = from(chosen); g < from(chosen + 1); ++g) {      // (all wavefronts walk the same quarter: the result is every thread's)
+    for (int g = from(chosen); g < from(chosen + 1); ++g) {
         const double s = sum_of(g);
         if (s > 0.0) {
             segment = g;
@@ -281,7 +318,7 @@ __device__ int64_t plain_token(const Verify& v, const Found& f, double u, int se
         }
         base += s;
     }
-    return token_of(v, weights, segment, target - before);
+    return token_of(weights, shards, segment, target - before);
 }
 
 template <typename T>
@@ -290,12 +327,8 @@ __global__ __launch_bounds__(THREADS) void verify_pick_kernel(Verify v, int segm
     __shared__ int chosen_segment;
     const int b = blockIdx.x, wave = threadIdx.x >> 6;
     const Rows rows(v, b);
-    if (!rows.any()) {
-        if (threadIdx.x == 0) v.accepted[b] = 0;
-        return;
-    }
-    const Found f = found[b];
-    const double u = v.uniforms[rows.last];
+    const Found f = found[b];      // (a sequence without rows has none, nor sums: what is read is not used)
+    const Lanes shards(v);
     // the segments, an equal number of neighbours to every thread
     part += (size_t)b * segments;
     const int each = (segments + THREADS - 1) / THREADS, g0 = threadIdx.x * each, g1 = min(segments, g0 + each);
@@ -303,8 +336,12 @@ __global__ __launch_bounds__(THREADS) void verify_pick_kernel(Verify v, int segm
     for (int g = g0; g < g1; ++g) mine += part[g];
     const double in_wave = wave_scan(mine);
     if ((threadIdx.x & 63) == 63) sums[wave] = in_wave;
-    if (threadIdx.x == 0) chosen_segment = -1;
     fill_table(table);
+    if (!rows.any()) {
+        if (threadIdx.x == 0) v.accepted[b] = 0;
+        return;
+    }
+    const double u = v.uniforms[rows.last];
     const double total = ((sums[0] + sums[1]) + sums[2]) + sums[3], target = u * total;
     int64_t token = -1;
     const bool rejected = f.at < rows.last;
@@ -338,10 +375,10 @@ __global__ __launch_bounds__(THREADS) void verify_pick_kernel(Verify v, int segm
             }
         }
         __syncthreads();
-        const Weights<T> weights(v, f, rejected, table);
-        token = token_of(v, weights, chosen_segment, target - chosen_base);
+        Weights<T> weights(v, f, rejected, table);
+        token = token_of(weights, shards, __builtin_amdgcn_readfirstlane(chosen_segment), target - chosen_base);
     } else if (total == 0.0 && rejected) {
-        token = plain_token<T>(v, f, u, segments, table, sums);
+        token = plain_token<T>(v, f, shards, u, segments, table, sums);
     }
     if (threadIdx.x == 0) v.accepted[b] = (int32_t)(f.at - rows.first);
     for (int64_t i = rows.first + threadIdx.x; i <= rows.last; i += THREADS)
