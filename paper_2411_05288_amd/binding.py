@@ -173,7 +173,7 @@ def load_library() -> ctypes.CDLL:
     lib.vp_profile_enable.argtypes = [c.c_int]
     lib.vp_profile_read.restype = c.c_int
     lib.vp_profile_read.argtypes = [c.POINTER(c.c_double), c.POINTER(c.c_int64), c.c_int]
-    for name in ("vp_block_norm_fwd", "vp_block_norm_bwd"):
+    for name in ("vp_block_norm_fwd", "vp_block_norm_bwd", "vp_quantize_rows", "vp_output_fwd_i8_group", "vp_verify_drafts"):
         _ADDRESS[name] = c.cast(getattr(lib, name), vp).value
     _LIB, _HOST = lib, host      # (only now: the native checks call the library's functions)
     return lib
@@ -743,6 +743,13 @@ def vp_i8_row_stride(h: int) -> int:
 def vp_quantize_rows(x, q, scales, stream=None) -> None:
     """Rows of x [N, h] in 8-bit integers: scales [N] = max |x| / 127, q [N, vp_i8_row_stride(h)] = 127 x / max |x| to the
     nearest integer, zero behind column h."""
+    if isinstance(stream, torch.cuda.Stream):
+        stream = stream.cuda_stream
+    if _HOST is not None:
+        st = _HOST.quantize_rows(_ADDRESS["vp_quantize_rows"], x, q, scales, stream)
+        if st is not None:      # the call was made
+            _check(st, "vp_quantize_rows")
+            return
     if x.dim() != 2:
         raise VPError("x must be [N, h]")
     N, h = x.shape
@@ -793,6 +800,14 @@ def vp_output_fwd_i8(H, H_scales, W_shard, W_scales, labels, shard_offset: int, 
 def vp_output_fwd_i8_group(H, H_scales, W_shards, W_scales, labels, shard_offsets, local_max, local_sumexp, local_target,
                            logits_out=None, workspace=None, stream=None) -> None:
     """vp_output_fwd_i8 for several shards on this device in one call; the statistics are [p, N]."""
+    if isinstance(stream, torch.cuda.Stream):
+        stream = stream.cuda_stream
+    if _HOST is not None:
+        st = _HOST.output_fwd_i8_group(_ADDRESS["vp_output_fwd_i8_group"], H, H_scales, W_shards, W_scales, labels, shard_offsets,
+                                       local_max, local_sumexp, local_target, logits_out, workspace, stream)
+        if st is not None:      # the call was made
+            _check(st, "vp_output_fwd_i8_group")
+            return
     if H.dim() != 2 or any(w.dim() != 2 for w in W_shards):
         raise VPError("H must be [N, k] and W_shards [rows, k]")
     N, k = H.shape
@@ -827,6 +842,14 @@ def vp_verify_drafts(logits, shard_offsets, global_max, global_sumexp, drafts, s
     """Verification of drafted tokens over the shards' logits ([N, rows] each) and the draw of the token behind them.  Sequence b
     has the rows starts[b] .. starts[b + 1] - 1, one for each draft and a last one; draft_*: the draft model's, row by row, or
     None (drafts that no model drew).  accepted [sequences] int32, tokens [N]: accepted drafts, the next token, -1 behind it."""
+    if isinstance(stream, torch.cuda.Stream):
+        stream = stream.cuda_stream
+    if _HOST is not None:
+        st = _HOST.verify_drafts(_ADDRESS["vp_verify_drafts"], logits, shard_offsets, global_max, global_sumexp, drafts, starts,
+                                 uniforms, accepted, tokens, workspace, draft_logits, draft_max, draft_sumexp, stream)
+        if st is not None:      # the call was made
+            _check(st, "vp_verify_drafts")
+            return
     if not logits or any(t.dim() != 2 for t in logits):
         raise VPError("logits must be [N, rows], a shard at least")
     N, p = logits[0].shape[0], len(logits)

@@ -190,6 +190,73 @@ struct Call {
         ok = true;
         return t.data_ptr();
     }
+    // the same for a type that the library has one name for
+    void* typed(PyObject* o, at::ScalarType type, std::initializer_list<int64_t> shape) {
+        if (o == Py_None || !ok) return nullptr;
+        ok = false;
+        if (!THPVariable_CheckExact(o)) return nullptr;
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!t.defined() || !t.is_cuda() || t.get_device() != here || !t.is_contiguous() || t.scalar_type() != type) return nullptr;
+        if (t.sizes() != at::IntArrayRef(shape.begin(), shape.size())) return nullptr;
+        ok = true;
+        return t.data_ptr();
+    }
+    // any contiguous tensor, and its bytes
+    void* memory(PyObject* o, size_t& bytes) {
+        if (!ok) return nullptr;
+        ok = false;
+        if (!THPVariable_CheckExact(o)) return nullptr;
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!t.defined() || !t.is_cuda() || t.get_device() != here || !t.is_contiguous()) return nullptr;
+        ok = true;
+        bytes = t.nbytes();
+        return t.data_ptr();
+    }
+    // the type of a list's first tensor
+    at::ScalarType type_of(PyObject* list) {
+        if (!PyList_Check(list) || PyList_GET_SIZE(list) < 1 || !THPVariable_CheckExact(PyList_GET_ITEM(list, 0))) {
+            ok = false;
+            return at::kFloat;
+        }
+        return THPVariable_Unpack(PyList_GET_ITEM(list, 0)).scalar_type();
+    }
+    // size d of every tensor of a list (at most `most`), which have `dims` dimensions
+    int sizes(PyObject* list, int64_t d, int64_t dims, int64_t* out, int most) {
+        if (!ok || !PyList_Check(list) || PyList_GET_SIZE(list) < 1 || PyList_GET_SIZE(list) > most) {
+            ok = false;
+            return 0;
+        }
+        const int n = (int)PyList_GET_SIZE(list);
+        for (int i = 0; i < n; ++i) {
+            PyObject* o = PyList_GET_ITEM(list, i);
+            if (!THPVariable_CheckExact(o) || !THPVariable_Unpack(o).defined() || THPVariable_Unpack(o).dim() != dims) {
+                ok = false;
+                return 0;
+            }
+            out[i] = THPVariable_Unpack(o).size(d);
+        }
+        return n;
+    }
+    // addresses of a list's n tensors: [rows[i]], [rows[i], other] or [other, rows[i]]
+    enum Shape { Vector, Rows, Columns };
+    void each(PyObject* list, int n, at::ScalarType type, const int64_t* rows, int64_t other, Shape shape, const void** out) {
+        if (!ok || !PyList_Check(list) || PyList_GET_SIZE(list) != n) {
+            ok = false;
+            return;
+        }
+        for (int i = 0; i < n; ++i) {
+            PyObject* o = PyList_GET_ITEM(list, i);
+            out[i] = shape == Vector ? typed(o, type, {rows[i]}) : shape == Rows ? typed(o, type, {rows[i], other}) : typed(o, type, {other, rows[i]});
+            if (!out[i]) ok = false;
+        }
+    }
+    void integers(PyObject* list, int n, int64_t* out) {
+        if (!ok || !PyList_Check(list) || PyList_GET_SIZE(list) != n) {
+            ok = false;
+            return;
+        }
+        for (int i = 0; i < n; ++i) out[i] = number((int64_t)PyLong_AsLongLong(PyList_GET_ITEM(list, i)));
+    }
     // N and h of a matrix; a gate's rows (0 for None; a gate without rows has no address and would be taken for none)
     int64_t size(PyObject* o, int64_t d) {
         if (o == Py_None) return 0;
@@ -290,7 +357,114 @@ PyObject* block_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return PyLong_FromLong(status);
 }
 
+using Quantize = int (*)(const void*, int64_t, int64_t, int, int8_t*, float*, void*);
+using LogitsI8 = int (*)(const void*, const void*, const void* const*, const void* const*, const int64_t*, const int64_t*, int32_t,
+                         const void*, int64_t, int64_t, int, uint32_t, void*, void*, void*, const void* const*, void*, size_t, void*);
+using Verify = int (*)(const void* const*, const int64_t*, const int64_t*, int32_t, int, const void*, const void*, const void* const*,
+                       const void*, const void*, const void*, const void*, const void*, int64_t, int32_t, void*, void*, void*, size_t,
+                       void*);
+constexpr int MOST = 64;      // shards
+
+// quantize_rows(function, x, q, scales, stream) -> status
+PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 5) Py_RETURN_NONE;
+    int status = 0;
+    try {
+        Call c;
+        const auto f = reinterpret_cast<Quantize>(c.pointer(a[0]));
+        const int64_t N = c.size(a[1], 0), h = c.size(a[1], 1);
+        if (!c.ok || a[1] == Py_None) Py_RETURN_NONE;
+        const int dt = c.dtype(a[1]);
+        void *x = c.at(a[1], dt, {N, h}), *q = c.typed(a[2], at::kChar, {N, (h + 127) / 128 * 128}), *scales = c.at(a[3], 0, {N});
+        void* stream = c.stream(a[4]);
+        if (!c.ok) Py_RETURN_NONE;
+        Py_BEGIN_ALLOW_THREADS
+        status = f(x, N, h, dt, static_cast<int8_t*>(q), static_cast<float*>(scales), stream);
+        Py_END_ALLOW_THREADS
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    return PyLong_FromLong(status);
+}
+
+// output_fwd_i8_group(function, H, H_scales, W_shards, W_scales, labels, shard_offsets, local_max, local_sumexp, local_target,
+//                     logits_out, workspace, stream) -> status
+PyObject* output_fwd_i8_group(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 13) Py_RETURN_NONE;
+    int status = 0;
+    try {
+        Call c;
+        const auto f = reinterpret_cast<LogitsI8>(c.pointer(a[0]));
+        const int64_t N = c.size(a[1], 0), k = c.size(a[1], 1);
+        if (!c.ok || a[1] == Py_None) Py_RETURN_NONE;
+        int64_t rows[MOST], offsets[MOST];
+        const void *W[MOST], *Ws[MOST], *Y[MOST];
+        const int p = c.sizes(a[3], 0, 2, rows, MOST);
+        void *H = c.typed(a[1], at::kChar, {N, k}), *Hs = c.at(a[2], 0, {N});
+        c.each(a[3], p, at::kChar, rows, k, Call::Rows, W);
+        c.each(a[4], p, at::kFloat, rows, 0, Call::Vector, Ws);
+        c.integers(a[6], p, offsets);
+        void *labels = c.typed(a[5], at::kLong, {N}), *m = c.at(a[7], 0, {p, N}), *s = c.at(a[8], 0, {p, N}), *t = c.at(a[9], 0, {p, N});
+        int dt = 1;
+        const bool keep = a[10] != Py_None;
+        if (keep) {
+            const at::ScalarType type = c.type_of(a[10]);
+            dt = vp_dtype_of(type);
+            if (dt < 0) Py_RETURN_NONE;
+            c.each(a[10], p, type, rows, N, Call::Columns, Y);
+        }
+        size_t bytes = 0;
+        void *workspace = c.memory(a[11], bytes), *stream = c.stream(a[12]);
+        if (!c.ok) Py_RETURN_NONE;
+        Py_BEGIN_ALLOW_THREADS
+        status = f(H, Hs, W, Ws, rows, offsets, p, labels, N, k, dt, keep ? 1 : 0, m, s, t, keep ? Y : nullptr, workspace, bytes, stream);
+        Py_END_ALLOW_THREADS
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    return PyLong_FromLong(status);
+}
+
+// verify_drafts(function, logits, shard_offsets, global_max, global_sumexp, drafts, starts, uniforms, accepted, tokens, workspace,
+//               draft_logits, draft_max, draft_sumexp, stream) -> status
+PyObject* verify_drafts(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 15) Py_RETURN_NONE;
+    int status = 0;
+    try {
+        Call c;
+        const auto f = reinterpret_cast<Verify>(c.pointer(a[0]));
+        int64_t rows[MOST], offsets[MOST];
+        const void *Y[MOST], *Z[MOST];
+        const int p = c.sizes(a[1], 1, 2, rows, MOST);
+        if (!c.ok || !THPVariable_CheckExact(a[6]) || !THPVariable_Unpack(a[6]).defined() || THPVariable_Unpack(a[6]).dim() != 1) Py_RETURN_NONE;
+        const int64_t N = THPVariable_Unpack(PyList_GET_ITEM(a[1], 0)).size(0), S = THPVariable_Unpack(a[6]).size(0) - 1;
+        const at::ScalarType type = c.type_of(a[1]);
+        const int dt = vp_dtype_of(type);
+        if (dt < 0 || S < 1 || S > INT32_MAX) Py_RETURN_NONE;
+        c.each(a[1], p, type, rows, N, Call::Columns, Y);
+        c.integers(a[2], p, offsets);
+        const bool model = a[11] != Py_None;
+        if (model) c.each(a[11], p, type, rows, N, Call::Columns, Z);
+        void *gmax = c.at(a[3], 0, {N}), *gsum = c.at(a[4], 0, {N}), *drafts = c.typed(a[5], at::kLong, {N});
+        void *starts = c.typed(a[6], at::kLong, {S + 1}), *u = c.at(a[7], 0, {N}), *accepted = c.typed(a[8], at::kInt, {S});
+        void *tokens = c.typed(a[9], at::kLong, {N}), *zmax = c.at(a[12], 0, {N}), *zsum = c.at(a[13], 0, {N});
+        size_t bytes = 0;
+        void *workspace = c.memory(a[10], bytes), *stream = c.stream(a[14]);
+        if (!c.ok) Py_RETURN_NONE;
+        Py_BEGIN_ALLOW_THREADS
+        status = f(Y, rows, offsets, p, dt, gmax, gsum, model ? Z : nullptr, zmax, zsum, drafts, starts, u, N, (int32_t)S, accepted, tokens,
+                   workspace, bytes, stream);
+        Py_END_ALLOW_THREADS
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    return PyLong_FromLong(status);
+}
+
 PyMethodDef methods[] = {
+    {"quantize_rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(quantize_rows)), METH_FASTCALL, nullptr},
+    {"output_fwd_i8_group", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(output_fwd_i8_group)), METH_FASTCALL, nullptr},
+    {"verify_drafts", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(verify_drafts)), METH_FASTCALL, nullptr},
     {"block_norm_fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(block_norm_fwd)), METH_FASTCALL, nullptr},
     {"block_norm_bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(block_norm_bwd)), METH_FASTCALL, nullptr},
     {"ptr", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(ptr)), METH_FASTCALL, nullptr},
