@@ -19,8 +19,13 @@ typedef unsigned uintx4u __attribute__((ext_vector_type(4), aligned(2)));
 //
 // A slot holds rows of 128 bytes, of W and then of H.  Chunk c of row r (16 bytes) sits at position c ^ (r / 2 % 8): 16
 // consecutive rows, which a read of LDS serves at a time, have the same chunk in 16 different groups of banks.
-constexpr int FEW_K = 128, FEW_SLOTS = 4;
-template <int TI, int WAVES>
+//
+// N=1 h=4096 V=128256: 92 us with the integers of H and the sums of the statistics (5.7 TB/s); 103 us with all workgroups at the
+// same k tile, whose lines lie in the same few memory channels; 116 us in the fast kernel.
+// Up to 64 tokens all sums, up to 128 the long ones: fast kernel -> this one, N=128 h=4096 V=128256 122 -> 110, h=8192 V=256000
+// 413 -> 391, N=65 h=4096 V=128256 112 -> 102.
+constexpr int FEW_K = 128, FEW_MOST = 128;
+template <int TI, int WAVES, int SLOTS>
 struct Few {
     static constexpr int COLS = 32 * WAVES, ROWS = 32 * TI, SLOT = (COLS + ROWS) * FEW_K;
     static constexpr int LOADS_W = COLS / 8 / WAVES, LOADS_H = (ROWS / 8 + WAVES - 1) / WAVES;
@@ -29,20 +34,23 @@ struct Few {
     static_assert(32 * STAGE_ROW <= SLOT, "staging exceeds a slot");
 };
 
-template <int TI, int WAVES>
+template <int TI, int WAVES, int SLOTS>
 __global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group gg) {
-    using F = Few<TI, WAVES>;
+    using F = Few<TI, WAVES, SLOTS>;
     __shared__ __attribute__((aligned(1024))) char slot0[F::SLOT];
     __shared__ __attribute__((aligned(1024))) char slot1[F::SLOT];
     __shared__ __attribute__((aligned(1024))) char slot2[F::SLOT];
-    __shared__ __attribute__((aligned(1024))) char slot3[F::SLOT];
-    static_assert(FEW_SLOTS == 4, "slots");
+    __shared__ __attribute__((aligned(1024))) char slot3[SLOTS == 4 ? F::SLOT : 16];
+    static_assert(SLOTS == 3 || SLOTS == 4, "slots");
     const GemmBf16Params& g = gg.base;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, hf = lane >> 5;
-    const int shard = shard_of(gg, blockIdx.x);
+    const int tiles_m = (g.M + F::ROWS - 1) / F::ROWS;
+    int tile_m, tile_n;
+    tile_of_block(blockIdx.x, gridDim.x, gridDim.x, tiles_m, gg.total, tile_m, tile_n);
+    const int shard = shard_of(gg, tile_n);
     const GemmBf16Shard& s = gg.sh[shard];
-    const int tile = (int)blockIdx.x - gg.first[shard], n0 = tile * F::COLS, k = g.K * 2;
+    const int m0 = tile_m * F::ROWS, n0 = (tile_n - gg.first[shard]) * F::COLS, k = g.K * 2;
     const unsigned w_bytes = (unsigned)s.rows * (unsigned)k, h_bytes = (unsigned)g.M * (unsigned)k;
 
     // this lane's columns are cbase + 8 (r / 4) + r % 4
@@ -54,7 +62,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group 
     for (int r = 0; r < 16; ++r) cs[r] = col_scales[min(cbase + 8 * (r >> 2) + (r & 3), s.rows - 1)];
 #pragma unroll
     for (int t = 0; t < TI; ++t) {
-        const int m = min(t * 32 + l32, g.M - 1);
+        const int m = min(m0 + t * 32 + l32, g.M - 1);
         rs[t] = gg.row_scales[m];
         label[t] = g.labels[m];
     }
@@ -68,10 +76,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group 
 #pragma unroll
     for (int i = 0; i < F::LOADS_H; ++i) {
         const int row = (wave * F::LOADS_H + i) * 8 + (lane >> 3), c = (lane & 7) ^ (row >> 1 & 7);
-        h_off[i] = (unsigned)row * (unsigned)k + (unsigned)c * 16u;
+        h_off[i] = (unsigned)(m0 + row) * (unsigned)k + (unsigned)c * 16u;
     }
     auto slot = [&](auto i) -> char* {
-        constexpr int S = decltype(i)::value % FEW_SLOTS;
+        constexpr int S = decltype(i)::value % SLOTS;
         if constexpr (S == 0) return slot0;
         else if constexpr (S == 1) return slot1;
         else if constexpr (S == 2) return slot2;
@@ -79,7 +87,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group 
     };
     // The k advance is applied to the descriptors: a k tile past the end has empty ones, no access is made and zeros arrive, as
     // they do for rows past the end of W or H.  Every workgroup begins at another k tile (sums of integers have no order).
-    const int nkt = k / FEW_K, turn = (int)(blockIdx.x) % nkt;
+    const int nkt = k / FEW_K, turn = tile_n % nkt;
     auto load = [&](auto i, int kt) {
         char* to = slot(i);
         const int at = kt + turn < nkt ? kt + turn : kt + turn - nkt;
@@ -112,16 +120,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group 
                 acc[t] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w, *reinterpret_cast<const intx4*>(from + h_at[kk] + t * 32 * FEW_K), acc[t], 0, 0, 0);
         }
     };
-    // k tile kt: its loads are the oldest of three tiles'; behind the barrier all wavefronts' have landed, and the slot of the tile
-    // before is free.
-    constexpr int PER = F::LOADS_W + F::LOADS_H;
-    static_assert(2 * PER < 64, "memory counter");
+    // k tile kt: its loads are the oldest of those on their way; behind the barrier all wavefronts' have landed, and the slot of the
+    // tile before is free.
+    constexpr int PER = F::LOADS_W + F::LOADS_H, LATER = (SLOTS - 2) * PER;
+    static_assert(LATER < 64, "memory counter");
     auto step = [&](auto i, int kt) {
-        __builtin_amdgcn_s_waitcnt(((2 * PER) & 15) | (((2 * PER) >> 4) << 14) | 0x70);      // vmcnt(2 PER), lgkmcnt(0)
+        __builtin_amdgcn_s_waitcnt((LATER & 15) | ((LATER >> 4) << 14) | 0x70);      // vmcnt(LATER), lgkmcnt(0)
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        load(std::integral_constant<int, decltype(i)::value + 3>{}, kt + 3);
+        load(std::integral_constant<int, decltype(i)::value + SLOTS - 1>{}, kt + SLOTS - 1);
         multiply(i);
     };
     constexpr std::integral_constant<int, 0> I0;
@@ -130,19 +138,19 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group 
     constexpr std::integral_constant<int, 3> I3;
     load(I0, 0);
     load(I1, 1);
-    load(I2, 2);
+    if constexpr (SLOTS == 4) load(I2, 2);
     int kt = 0;
-    for (int it = nkt / 4; it > 0; --it, kt += 4) {
+    for (int it = nkt / SLOTS; it > 0; --it, kt += SLOTS) {
         step(I0, kt);
         step(I1, kt + 1);
         step(I2, kt + 2);
-        step(I3, kt + 3);
+        if constexpr (SLOTS == 4) step(I3, kt + 3);
     }
     if (kt < nkt) {
         step(I0, kt);
         if (kt + 1 < nkt) {
             step(I1, kt + 1);
-            if (kt + 2 < nkt) step(I2, kt + 2);
+            if (SLOTS == 4 && kt + 2 < nkt) step(I2, kt + 2);
         }
     }
     __syncthreads();      // no load is in flight, and no wavefront reads a slot
@@ -151,8 +159,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group 
 
 #pragma unroll
     for (int t = 0; t < TI; ++t) {
-        if (t * 32 >= g.M) break;
-        const int m = t * 32 + l32;
+        if (m0 + t * 32 >= g.M) break;
+        const int lm = t * 32 + l32, m = m0 + lm;
         float y[16], v = -INFINITY;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -165,8 +173,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group 
         for (int r = 0; r < 16; ++r) sum += exp2_fast((y[r] - v) * LOG2E);
         sum += __shfl_xor(sum, 32, 64);
         if (hf == 0) {
-            xm[wave][m] = v;
-            xs[wave][m] = sum;
+            xm[wave][lm] = v;
+            xs[wave][lm] = sum;
         }
         const int64_t at = label[t] - s.offset - cbase;
         if (label[t] >= 0 && at >= 0 && at < 32 && (at & 4) == 0 && at + cbase < s.rows && m < g.M) {
@@ -178,7 +186,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group 
         }
         if (s.out) {
             if (t) __syncthreads();
-            const int cols = min(F::COLS, s.rows - n0), rows = min(32, g.M - t * 32);
+            const int cols = min(F::COLS, s.rows - n0), rows = min(32, g.M - m0 - t * 32);
             const int elem = gg.out_f32 ? 4 : 2, per_row = F::COLS * elem / 16;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -190,7 +198,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group 
             for (int i = threadIdx.x; i < rows * per_row; i += 64 * WAVES) {
                 const int row = i / per_row, c = i % per_row * (16 / elem);
                 const char* from = slot0 + row * F::STAGE_ROW + c * elem;
-                char* to = (char*)s.out + ((size_t)(t * 32 + row) * s.ld + n0 + c) * elem;
+                char* to = (char*)s.out + ((size_t)(m0 + t * 32 + row) * s.ld + n0 + c) * elem;
                 if (c + 16 / elem <= cols) *reinterpret_cast<uintx4u*>(to) = *reinterpret_cast<const uintx4*>(from);
                 else
                     for (int e = 0; c + e < cols; ++e) {
@@ -201,16 +209,123 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group 
         }
     }
     __syncthreads();
-    for (int m = threadIdx.x; m < F::ROWS && m < g.M; m += 64 * WAVES) {
+    for (int m = threadIdx.x; m < F::ROWS && m0 + m < g.M; m += 64 * WAVES) {
         float v = xm[0][m], sum = 0.f;
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) v = fmaxf(v, xm[w][m]);
 #pragma unroll
         for (int w = 0; w < WAVES; ++w)
             if (xm[w][m] > -INFINITY) sum += xs[w][m] * __expf(xm[w][m] - v);
-        g.part_max[(size_t)blockIdx.x * g.M + m] = v;
-        g.part_sum[(size_t)blockIdx.x * g.M + m] = sum;
+        g.part_max[(size_t)tile_n * g.M + m0 + m] = v;
+        g.part_sum[(size_t)tile_n * g.M + m0 + m] = sum;
     }
+}
+
+// Tiles of 128 tokens and 256 vocabulary rows, two workgroups on a compute unit, so that one multiplies while the other is at its
+// ends: where the sum is short, the statistics and stores of a tile take as long as its products.  A ring of three slots of 64
+// integers (A's 128 rows, then B's 256, 64 bytes each, laid out as in vp_gemm_bf16_fast.h), one multiplied while two are on their
+// way, one barrier per slot.
+// Where it is taken: sums of up to PAIR_MOST_K integers.  The fast kernel -> this one, us: N=509 h=1001 V=50001 fp32 76 -> 57, N=1000
+// h=1536 V=50001 bf16 129 -> 111, N=4096 h=1024 V=32000 224 -> 182, h=2048 V=64000 647 -> 638, h=2560 V=64000 746 -> 791.
+// STREAM: outputs bypass the caches where there is more than one round of tiles, as in the fast kernel, but not fp32 rows that
+// share lines (N=509 h=1001 V=50001 in 3 shards: 78 us with it, 57 without; in whole lines, V=49152, 50 and 51).
+constexpr int PAIR_MOST_K = 2048;
+constexpr int PAIR_ROWS = 128, PAIR_K = 64, PAIR_SLOT = (PAIR_ROWS + BN) * PAIR_K;
+static_assert(2 * StageF32<64>::BYTES <= PAIR_SLOT && StageBf16<128>::BYTES <= StageF32<64>::BYTES, "staging of two wavefronts exceeds a slot");
+
+template <bool STREAM>
+__global__ __launch_bounds__(256, 2) void gemm_i8_pair_kernel(GemmI8Group gg) {
+    __shared__ __attribute__((aligned(1024))) char slot0[PAIR_SLOT];
+    __shared__ __attribute__((aligned(1024))) char slot1[PAIR_SLOT];
+    __shared__ __attribute__((aligned(1024))) char slot2[PAIR_SLOT];
+    __shared__ __attribute__((aligned(16))) char xchg[EPI_XCHG_BYTES];
+    const GemmBf16Params& g = gg.base;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave >> 1, wn = wave & 1;
+    const int tiles_m = (g.M + PAIR_ROWS - 1) / PAIR_ROWS;
+    int tile_m, tile_n;
+    tile_of_block(blockIdx.x, gridDim.x, gridDim.x, tiles_m, gg.total, tile_m, tile_n);
+    const int shard = shard_of(gg, tile_n);
+    tile_n -= gg.first[shard];
+    const GemmBf16Shard& s = gg.sh[shard];
+    const int m0 = tile_m * PAIR_ROWS, n0 = tile_n * BN;
+    const unsigned a_bytes = (unsigned)g.M * (unsigned)g.lda * 2u, b_bytes = (unsigned)s.rows * (unsigned)g.ldb * 2u;
+    I8Inputs in;
+    in.load(g, gg.row_scales, gg.col_scales[shard], m0, n0, s.rows);
+
+    unsigned avoff[2], bvoff[4];
+    half_voffsets<true, 2>(avoff, m0, g.lda, wave, lane);
+    half_voffsets<true, 4>(bvoff, n0, g.ldb, wave, lane);
+    int abase[4], bbase[4];
+    frag_offsets<true, 2>(abase, wm, lane);
+    frag_offsets<true>(bbase, wn, lane);
+    auto slot = [&](auto i) -> char* {
+        constexpr int S = decltype(i)::value % 3;
+        if constexpr (S == 0) return slot0;
+        else if constexpr (S == 1) return slot1;
+        else return slot2;
+    };
+    const int steps = g.K * 2 / PAIR_K;
+    auto load = [&](auto i, int at) {      // (past the end: empty descriptors, see gemm_i8_few_kernel)
+        char* to = slot(i);
+        const unsigned adv = at < steps ? (unsigned)(at * PAIR_K) : ~0u, aa = min(adv, a_bytes), ba = min(adv, b_bytes);
+        const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)g.A + aa), 0, (int)(a_bytes - aa), 0x00020000);
+        const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)s.B + ba), 0, (int)(b_bytes - ba), 0x00020000);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_ptr)(to + (wave * 2 + j) * 1024), 16, (int)avoff[j], 0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_ptr)(to + PAIR_ROWS * PAIR_K + (wave * 4 + j) * 1024), 16, (int)bvoff[j], 0, 0, 0);
+    };
+    floatx16 acc[2][4] = {};
+    auto multiply = [&](auto i) {
+        const char* from = slot(i);
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            bf16x8 a[2], b[4];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) a[t] = read_operand<true>(from, abase, t, kk);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) b[t] = read_operand<true>(from + PAIR_ROWS * PAIR_K, bbase, t, kk);
+            mfma_step<Epi::LogitsI8, 2>(acc, a, b);
+        }
+    };
+    auto step = [&](auto i, int at) {
+        __builtin_amdgcn_s_waitcnt(6 | 0x70);      // vmcnt(6): all but the last slot's loads; lgkmcnt(0)
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        load(std::integral_constant<int, decltype(i)::value + 2>{}, at + 2);
+        multiply(i);
+    };
+    constexpr std::integral_constant<int, 0> I0;
+    constexpr std::integral_constant<int, 1> I1;
+    constexpr std::integral_constant<int, 2> I2;
+    load(I0, 0);
+    load(I1, 1);
+    int at = 0;
+    for (int it = steps / 3; it > 0; --it, at += 3) {
+        step(I0, at);
+        step(I1, at + 1);
+        step(I2, at + 2);
+    }
+    if (at < steps) {
+        step(I0, at);
+        if (at + 1 < steps) step(I1, at + 1);
+    }
+    __syncthreads();
+
+    GemmBf16Params e = g;
+    e.N = s.rows;
+    e.Y = (u16*)s.out;
+    e.ldy = s.ld;
+    e.shard_offset = s.offset;
+    e.part_max = g.part_max + (size_t)gg.first[shard] * g.M;
+    e.part_sum = g.part_sum + (size_t)gg.first[shard] * g.M;
+    e.part_tgt = g.part_tgt + (size_t)shard * g.M;
+    char* region = (wave < 2 ? slot0 : slot1) + (wave & 1) * StageF32<64>::BYTES;
+    gemm_epilogue_i8<STREAM, 2, 64>(acc, e, gg.out_f32, in, tile_m, tile_n, xchg, region);
 }
 
 }  // namespace
@@ -228,9 +343,19 @@ hipError_t launch_gemm_i8(const GemmI8Group& g0, hipStream_t st) {
         if (r < g.n) g.total += (int)ceil_div(g.sh[r].rows, cols);
     }
     g.slices = 1;
-    if (g.base.M > 64) return launch_fast_t<true, true, Epi::LogitsI8>(g, st);
-    if (g.base.M <= 32) hipLaunchKernelGGL((gemm_i8_few_kernel<1, 4>), dim3(g.total), dim3(256), 0, st, g);
-    else hipLaunchKernelGGL((gemm_i8_few_kernel<2, 4>), dim3(g.total), dim3(256), 0, st, g);
+    auto few = [&](auto kernel, int rows, int waves) {
+        hipLaunchKernelGGL(kernel, dim3(g.total * (int)ceil_div(g.base.M, rows)), dim3(64 * waves), 0, st, g);
+        return hipGetLastError();
+    };
+    if (g.base.M <= 32) return few(gemm_i8_few_kernel<1, 4, 4>, 32, 4);
+    if (g.base.M <= 64) return few(gemm_i8_few_kernel<2, 4, 4>, 64, 4);
+    if (g.base.M <= FEW_MOST && g.base.K * 2 > PAIR_MOST_K) return few(gemm_i8_few_kernel<4, 8, 3>, 128, 8);
+    if (g.base.K * 2 > PAIR_MOST_K) return launch_fast_t<true, true, Epi::LogitsI8>(g, st);
+    const int tiles = g.total * (int)ceil_div(g.base.M, PAIR_ROWS);
+    bool stream = tiles > 2 * compute_unit_count();
+    for (int r = 0; r < g.n; ++r) stream &= !(g.out_f32 && g.sh[r].ld % 16);
+    if (stream) hipLaunchKernelGGL(gemm_i8_pair_kernel<true>, dim3(tiles), dim3(256), 0, st, g);
+    else hipLaunchKernelGGL(gemm_i8_pair_kernel<false>, dim3(tiles), dim3(256), 0, st, g);
     return hipGetLastError();
 }
 

@@ -52,7 +52,8 @@ __device__ __forceinline__ void flush_stage_f32(const char* region, __amdgpu_buf
     }
 }
 
-template <bool STREAM, int MI>
+// F32_COLS: fp32 outputs are staged 128 or 64 columns at a time (a region of 16.5 or 8.5 KB).
+template <bool STREAM, int MI, int F32_COLS = 128>
 __device__ __forceinline__ void gemm_epilogue_i8(floatx16 (&acc)[MI][4], const GemmBf16Params& g, int out_f32, const I8Inputs& in,
                                                  int tile_m, int tile_n, char* xchg, char* region) {
     constexpr int NJ = 4, WN = 2, WCOLS = 128, TM = 64 * MI;
@@ -82,17 +83,14 @@ __device__ __forceinline__ void gemm_epilogue_i8(floatx16 (&acc)[MI][4], const G
     // OUT: 0 the statistics alone, 1 bf16, 2 fp32
     auto blocks = [&](auto out_c) {
         constexpr int OUT = decltype(out_c)::value;
-        typedef typename std::conditional<OUT == 2, StageF32<WCOLS>, StageBf16<WCOLS>>::type St;
+        constexpr int SCOLS = OUT == 2 ? F32_COLS : WCOLS, PARTS = WCOLS / SCOLS, PJ = NJ / PARTS;
+        typedef typename std::conditional<OUT == 2, StageF32<SCOLS>, StageBf16<SCOLS>>::type St;
         constexpr int ELEM = OUT == 2 ? 4 : 2, PER = 16 / ELEM;
         const int orow = lane / St::LPR, ochunk = lane % St::LPR;
-        const int ocol = n0 + wn * WCOLS + ochunk * PER;
         const unsigned row_bytes = (unsigned)g.ldy * (unsigned)ELEM;
         const __amdgpu_buffer_rsrc_t rs =
             tile_rows_rsrc(OUT ? (char*)g.Y + (size_t)m0 * g.ldy * ELEM : nullptr, OUT ? (g.M - m0 < TM ? g.M - m0 : TM) : 0, row_bytes);
-        const unsigned off_row = (unsigned)(wm * (32 * MI) + orow) * row_bytes + (unsigned)ocol * (unsigned)ELEM;
-        const unsigned off0 = ocol + PER <= g.N ? off_row : OOB_OFFSET;
         const bool tail = n0 + WN * WCOLS > g.N && g.N % PER != 0;
-        const int n_tail = ocol + PER > g.N && ocol < g.N ? g.N - ocol : 0;
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             __builtin_amdgcn_sched_barrier(0);      // one row block at a time (see gemm_epilogue_bf16)
@@ -146,22 +144,28 @@ __device__ __forceinline__ void gemm_epilogue_i8(floatx16 (&acc)[MI][4], const G
             }
             if constexpr (OUT) {
 #pragma unroll
-                for (int j = 0; j < NJ; ++j)
+                for (int part = 0; part < PARTS; ++part) {
+                    const int ocol = n0 + wn * WCOLS + part * SCOLS + ochunk * PER;
+                    const unsigned off_row = (unsigned)(wm * (32 * MI) + i * 32 + orow) * row_bytes + (unsigned)ocol * (unsigned)ELEM;
+                    const unsigned off = ocol + PER <= g.N ? off_row : OOB_OFFSET;
+                    const int n_tail = ocol + PER > g.N && ocol < g.N ? g.N - ocol : 0;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        float y[4];
+                    for (int j = 0; j < PJ; ++j)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) y[e] = acc[i][j][4 * q + e] * scale;
-                        char* to = region + l32 * St::RS + (j * 32 + 8 * q + 4 * hf) * ELEM;
-                        if constexpr (OUT == 2) *reinterpret_cast<floatx4*>(to) = floatx4{y[0], y[1], y[2], y[3]};
-                        else *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
-                    }
-                wave_lds_fence();
-                const unsigned down = (unsigned)(i * 32) * row_bytes;
-                const int left = g.M - (m0 + wm * (32 * MI) + i * 32);
-                if constexpr (OUT == 2) flush_stage_f32<St, STREAM>(region, rs, off0 + down, row_bytes, orow, ochunk, tail, off_row + down, n_tail, left);
-                else flush_stage_bf16<St, STREAM>(region, rs, off0 + down, row_bytes, orow, ochunk, tail, off_row + down, n_tail, left);
-                wave_lds_fence();
+                        for (int q = 0; q < 4; ++q) {
+                            float y[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) y[e] = acc[i][part * PJ + j][4 * q + e] * scale;
+                            char* to = region + l32 * St::RS + (j * 32 + 8 * q + 4 * hf) * ELEM;
+                            if constexpr (OUT == 2) *reinterpret_cast<floatx4*>(to) = floatx4{y[0], y[1], y[2], y[3]};
+                            else *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
+                        }
+                    wave_lds_fence();
+                    const int left = g.M - (m0 + wm * (32 * MI) + i * 32);
+                    if constexpr (OUT == 2) flush_stage_f32<St, STREAM>(region, rs, off, row_bytes, orow, ochunk, tail, off_row, n_tail, left);
+                    else flush_stage_bf16<St, STREAM>(region, rs, off, row_bytes, orow, ochunk, tail, off_row, n_tail, left);
+                    wave_lds_fence();
+                }
             }
         }
     };
