@@ -325,7 +325,7 @@ __global__ __launch_bounds__(256, 2) void gemm_i8_pair_kernel(GemmI8Group gg) {
     e.part_sum = g.part_sum + (size_t)gg.first[shard] * g.M;
     e.part_tgt = g.part_tgt + (size_t)shard * g.M;
     char* region = (wave < 2 ? slot0 : slot1) + (wave & 1) * StageF32<64>::BYTES;
-    gemm_epilogue_i8<STREAM, 2, 64>(acc, e, gg.out_f32, in, tile_m, tile_n, xchg, region);
+    gemm_epilogue_i8<STREAM, 2, false>(acc, e, gg.out_f32, in, tile_m, tile_n, xchg, region);
 }
 
 }  // namespace
