@@ -770,8 +770,8 @@ def vp_output_i8_workspace_bytes(N: int, rows) -> int:
 def _logits_code(logits_out) -> int:
     if logits_out is None:
         return VP_BF16
-    if any(t.dtype != logits_out[0].dtype for t in logits_out):
-        raise VPError("logits_out: tensors of one type")
+    if not logits_out or any(t.dtype != logits_out[0].dtype for t in logits_out):
+        raise VPError("logits_out: a tensor for each shard, of one type")
     return _dtype_code(logits_out[0])
 
 

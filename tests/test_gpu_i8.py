@@ -181,6 +181,23 @@ def test_lengths_of_the_sum(N, k):
     case.check(case.run())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [1, 64, 65, 96, 97, 128, 129, 192, 193, 256, 300, 513])
+@pytest.mark.parametrize("k,rows", [(2048, [300, 5]), (2176, [300, 5]), (2304, [1, 255, 257]), (4096, [513, 1000])])
+def test_long_sums(N, k, rows, dtype):
+    """On both sides of every choice between the kernels: sums of 2048, 64 and 128 tokens, tiles of 64 to 256 tokens."""
+    case = Product(N, k, rows, dtype, seed=N + k)
+    case.check(case.run())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,k,rows", [(300, 128, [25000, 26001]), (300, 128, [25600, 25600]), (300, 2304, [20001, 20002]),
+                                      (2200, 128, [3000, 3001]), (2200, 2304, [3001]), (40, 256, [70001]), (100, 2304, [70001])])
+def test_more_tiles_than_compute_units(N, k, rows, dtype):
+    case = Product(N, k, rows, dtype, seed=k)
+    case.check(case.run())
+
+
 @pytest.mark.parametrize("N,k,rows", [(1, 128, [1]), (3, 128, [7] * 20), (5, 256, [64] * 16), (40, 256, [300] * 17), (300, 128, [100] * 40)])
 def test_many_shards(N, k, rows):
     case = Product(N, k, rows, "bf16", seed=5)
@@ -271,6 +288,20 @@ def test_repeats_bit_for_bit():
     assert all(torch.equal(x, y) for x, y in zip((*a[:3], *a[3]), (*b[:3], *b[3])))
 
 
+@pytest.mark.parametrize("N", [1, 40, 100])
+def test_the_checks_in_python_lead_to_the_same_calls(N, monkeypatch):
+    import paper_2411_05288_amd.binding as B
+    B.load_library()
+    case = Product(N, 256, [300, 77], "bf16", seed=4)
+    x = torch.randn(N, 200, generator=torch.Generator().manual_seed(1)).cuda()
+    native, rows = case.run(), quantize(x)
+    assert B._HOST is not None
+    monkeypatch.setattr(B, "_HOST", None)
+    python, same_rows = case.run(), quantize(x)
+    assert all(torch.equal(a, b) for a, b in zip((*native[:3], *native[3]), (*python[:3], *python[3])))
+    assert (rows[0] == same_rows[0]).all() and (rows[1] == same_rows[1]).all()
+
+
 def test_python_refusals():
     import paper_2411_05288_amd as vp
     z = lambda *s, dtype=torch.float32: torch.zeros(*s, dtype=dtype, device="cuda")      # noqa: E731
@@ -286,6 +317,8 @@ def test_python_refusals():
     for bad in (dict(H=i8(4, 256)), dict(H=z(4, 128)), dict(H_scales=z(5)), dict(W_shards=[i8(30, 128)]), dict(W_scales=[z(30)]),
                 dict(W_scales=[z(30), z(21)]), dict(shard_offsets=[0]), dict(labels=z(4)), dict(local_max=z(1, 4)),
                 dict(logits_out=[z(4, 30)]), dict(logits_out=[z(4, 30), z(4, 21)]), dict(workspace=None),
-                dict(logits_out=[z(4, 30), z(4, 20, dtype=torch.bfloat16)]), dict(H=i8(128, 4).t()), dict(H=i8(128))):
+                dict(logits_out=[z(4, 30), z(4, 20, dtype=torch.bfloat16)]), dict(H=i8(128, 4).t()), dict(H=i8(128)),
+                dict(logits_out=[]), dict(logits_out=[z(4, 30, dtype=torch.float16), z(4, 20, dtype=torch.float16)]),
+                dict(W_shards=[], W_scales=[], shard_offsets=[], logits_out=None), dict(local_max=good["local_sumexp"])):
         with pytest.raises(vp.VPError):
             vp.vp_output_fwd_i8_group(**{**good, **bad})

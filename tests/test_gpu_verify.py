@@ -289,6 +289,57 @@ def test_logits_that_start_at_any_element():
     np.testing.assert_array_equal(a["tokens"].cpu().numpy(), c.want()[1])
 
 
+@pytest.mark.parametrize("model", [True, False])
+def test_the_checks_in_python_lead_to_the_same_call(model, monkeypatch):
+    import paper_2411_05288_amd.binding as B
+    B.load_library()
+    c = Case([2, 0, 5, 1], [300, 77], "bf16", model)
+    native = c.check()
+    assert B._HOST is not None
+    monkeypatch.setattr(B, "_HOST", None)
+    for a, b in zip(native, c.run()):
+        np.testing.assert_array_equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("model", [True, False])
+def test_many_sequences_of_a_large_vocabulary(model, dtype):
+    """More segments than wavefronts on the chip: the token is checked by its place in the running sum of 64 bits."""
+    import paper_2411_05288_amd as vp
+    S, rows = 700, [6500, 6501]
+    N, V = 2 * S, sum(rows)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    Y = [(2 * torch.randn(N, n, generator=gen, device="cuda")).to(TYPES[dtype]) for n in rows]
+    Z = [(y.float() + 0.5 * torch.randn(N, y.shape[1], generator=gen, device="cuda")).to(TYPES[dtype]) for y in Y] if model else None
+
+    def stats(shards):
+        m = torch.cat(shards, 1).float().amax(1)
+        return m, torch.exp(torch.cat(shards, 1).double() - m[:, None].double()).sum(1).float()
+    (m, s), (zm, zs) = stats(Y), stats(Z) if model else (None, None)
+    drafts = torch.randint(0, V, (N,), generator=gen, device="cuda")
+    starts = torch.arange(0, N + 1, 2, device="cuda")
+    u = torch.rand(N, generator=gen, device="cuda")
+    accepted, tokens = torch.empty(S, dtype=torch.int32, device="cuda"), torch.empty(N, dtype=torch.int64, device="cuda")
+    ws = torch.full((vp.vp_verify_workspace_bytes(S, V),), 0xFF, dtype=torch.uint8, device="cuda")
+    vp.vp_verify_drafts(Y, [0, rows[0]], m, s, drafts, starts, u, accepted, tokens, ws, draft_logits=Z, draft_max=zm, draft_sumexp=zs)
+    first = torch.arange(0, N, 2, device="cuda")
+    p = torch.exp(torch.cat(Y, 1).double() - m[:, None].double()) / s[:, None].double()
+    q = torch.exp(torch.cat(Z, 1).double() - zm[:, None].double()) / zs[:, None].double() if model else torch.nn.functional.one_hot(drafts, V).double()
+    d = drafts[first]
+    ok = u[first].double() * q[first, d] < p[first, d]
+    assert torch.equal(accepted, ok.int())
+    w = torch.where(ok[:, None], p[first + 1], (p[first] - q[first]).clamp(min=0))
+    c = w.cumsum(1)
+    token = tokens[torch.where(ok, first + 1, first)]
+    target = u[first + 1].double() * c[:, -1]
+    upto = c.gather(1, token[:, None])[:, 0]
+    before = upto - w.gather(1, token[:, None])[:, 0]
+    # sums of 13001 terms in 64 bits: off by less than 1e-11 of the whole
+    assert bool((before <= target + 1e-11 * c[:, -1]).all()) and bool((upto >= target - 1e-11 * c[:, -1]).all())
+    assert bool((w.gather(1, token[:, None]) > 0).all())
+    assert bool((tokens[first[ok]] == d[ok]).all()) and bool((tokens[first[~ok] + 1] == -1).all())
+
+
 def test_python_refusals():
     import paper_2411_05288_amd as vp
     c = Case([2, 3], [77, 31], "bf16")
