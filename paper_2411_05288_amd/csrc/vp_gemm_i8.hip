@@ -1,6 +1,7 @@
 // The output layer's logits from 8-bit integers.  Many tokens: the fast kernel (vp_gemm_bf16_fast.h) with integer products, whose
-// operands of 16 bytes hold 16 integers in place of 8 numbers; data movement, tiles and tile order are the same.  Few tokens: a
-// kernel of its own, below, that is bound by reading W.
+// operands of 16 bytes hold 16 integers in place of 8 numbers; data movement, tiles and tile order are the same.  It is bound by the
+// power limit, like the bf16 products (main loops at 1.5 to 1.7 GHz of 2.4): N=4096 h=8192 V=256000 2.5 POP/s, h=4096 V=128256
+// 2.4.  Short sums: tiles in pairs, bound by their statistics and stores.  Few tokens: a kernel that is bound by reading W.
 #include <climits>
 
 #include "vp_gemm_bf16_fast.h"
@@ -9,7 +10,6 @@ namespace vp {
 
 namespace {
 
-typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef unsigned uintx4u __attribute__((ext_vector_type(4), aligned(2)));
 
 // Few tokens: 32 TI of them and 32 WAVES vocabulary rows in a workgroup of WAVES wavefronts, which take 32 rows each.  W is read
@@ -20,8 +20,8 @@ typedef unsigned uintx4u __attribute__((ext_vector_type(4), aligned(2)));
 // A slot holds rows of 128 bytes, of W and then of H.  Chunk c of row r (16 bytes) sits at position c ^ (r / 2 % 8): 16
 // consecutive rows, which a read of LDS serves at a time, have the same chunk in 16 different groups of banks.
 //
-// N=1 h=4096 V=128256: 92 us with the integers of H and the sums of the statistics (5.7 TB/s); 103 us with all workgroups at the
-// same k tile, whose lines lie in the same few memory channels; 116 us in the fast kernel.
+// N=1 h=4096 V=128256: 78 us (6.7 TB/s).  With the integers of H and the fold 87 us; 116 in the fast kernel; where all workgroups
+// begin at the same k tile, whose lines lie in the same few memory channels, 11 more.
 // Up to 64 tokens all sums, up to 128 the long ones: fast kernel -> this one, N=128 h=4096 V=128256 122 -> 110, h=8192 V=256000
 // 413 -> 391, N=65 h=4096 V=128256 112 -> 102.
 constexpr int FEW_K = 128, FEW_MOST = 128;
@@ -45,12 +45,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group 
     const GemmBf16Params& g = gg.base;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, hf = lane >> 5;
-    const int tiles_m = (g.M + F::ROWS - 1) / F::ROWS;
-    int tile_m, tile_n;
-    tile_of_block(blockIdx.x, gridDim.x, gridDim.x, tiles_m, gg.total, tile_m, tile_n);
+    int tile_m, tile_n;      // (one row of tiles)
+    tile_of_block(blockIdx.x, gridDim.x, gridDim.x, 1, gg.total, tile_m, tile_n);
     const int shard = shard_of(gg, tile_n);
     const GemmBf16Shard& s = gg.sh[shard];
-    const int m0 = tile_m * F::ROWS, n0 = (tile_n - gg.first[shard]) * F::COLS, k = g.K * 2;
+    const int n0 = (tile_n - gg.first[shard]) * F::COLS, k = g.K * 2;
     const unsigned w_bytes = (unsigned)s.rows * (unsigned)k, h_bytes = (unsigned)g.M * (unsigned)k;
 
     // this lane's columns are cbase + 8 (r / 4) + r % 4
@@ -62,7 +61,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group 
     for (int r = 0; r < 16; ++r) cs[r] = col_scales[min(cbase + 8 * (r >> 2) + (r & 3), s.rows - 1)];
 #pragma unroll
     for (int t = 0; t < TI; ++t) {
-        const int m = min(m0 + t * 32 + l32, g.M - 1);
+        const int m = min(t * 32 + l32, g.M - 1);
         rs[t] = gg.row_scales[m];
         label[t] = g.labels[m];
     }
@@ -76,7 +75,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group 
 #pragma unroll
     for (int i = 0; i < F::LOADS_H; ++i) {
         const int row = (wave * F::LOADS_H + i) * 8 + (lane >> 3), c = (lane & 7) ^ (row >> 1 & 7);
-        h_off[i] = (unsigned)(m0 + row) * (unsigned)k + (unsigned)c * 16u;
+        h_off[i] = (unsigned)row * (unsigned)k + (unsigned)c * 16u;
     }
     auto slot = [&](auto i) -> char* {
         constexpr int S = decltype(i)::value % SLOTS;
@@ -153,14 +152,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group 
             if (SLOTS == 4 && kt + 2 < nkt) step(I2, kt + 2);
         }
     }
-    __syncthreads();      // no load is in flight, and no wavefront reads a slot
+    __builtin_amdgcn_s_waitcnt(0x0F70);      // vmcnt(0): nor do zeros past the end arrive in a slot any more
+    __syncthreads();      // no wavefront reads a slot
     // the statistics of the wavefronts' columns; outputs are staged in slot 0
     float(*xm)[F::ROWS] = reinterpret_cast<float(*)[F::ROWS]>(slot1), (*xs)[F::ROWS] = xm + WAVES;
 
 #pragma unroll
     for (int t = 0; t < TI; ++t) {
-        if (m0 + t * 32 >= g.M) break;
-        const int lm = t * 32 + l32, m = m0 + lm;
+        if (t * 32 >= g.M) break;
+        const int m = t * 32 + l32;
         float y[16], v = -INFINITY;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -173,8 +173,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group 
         for (int r = 0; r < 16; ++r) sum += exp2_fast((y[r] - v) * LOG2E);
         sum += __shfl_xor(sum, 32, 64);
         if (hf == 0) {
-            xm[wave][lm] = v;
-            xs[wave][lm] = sum;
+            xm[wave][m] = v;
+            xs[wave][m] = sum;
         }
         const int64_t at = label[t] - s.offset - cbase;
         if (label[t] >= 0 && at >= 0 && at < 32 && (at & 4) == 0 && at + cbase < s.rows && m < g.M) {
@@ -186,7 +186,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group 
         }
         if (s.out) {
             if (t) __syncthreads();
-            const int cols = min(F::COLS, s.rows - n0), rows = min(32, g.M - m0 - t * 32);
+            const int cols = min(F::COLS, s.rows - n0), rows = min(32, g.M - t * 32);
             const int elem = gg.out_f32 ? 4 : 2, per_row = F::COLS * elem / 16;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -198,7 +198,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group 
             for (int i = threadIdx.x; i < rows * per_row; i += 64 * WAVES) {
                 const int row = i / per_row, c = i % per_row * (16 / elem);
                 const char* from = slot0 + row * F::STAGE_ROW + c * elem;
-                char* to = (char*)s.out + ((size_t)(m0 + t * 32 + row) * s.ld + n0 + c) * elem;
+                char* to = (char*)s.out + ((size_t)(t * 32 + row) * s.ld + n0 + c) * elem;
                 if (c + 16 / elem <= cols) *reinterpret_cast<uintx4u*>(to) = *reinterpret_cast<const uintx4*>(from);
                 else
                     for (int e = 0; c + e < cols; ++e) {
@@ -209,15 +209,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group 
         }
     }
     __syncthreads();
-    for (int m = threadIdx.x; m < F::ROWS && m0 + m < g.M; m += 64 * WAVES) {
+    for (int m = threadIdx.x; m < g.M; m += 64 * WAVES) {
         float v = xm[0][m], sum = 0.f;
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) v = fmaxf(v, xm[w][m]);
 #pragma unroll
         for (int w = 0; w < WAVES; ++w)
             if (xm[w][m] > -INFINITY) sum += xs[w][m] * __expf(xm[w][m] - v);
-        g.part_max[(size_t)tile_n * g.M + m0 + m] = v;
-        g.part_sum[(size_t)tile_n * g.M + m0 + m] = sum;
+        g.part_max[(size_t)tile_n * g.M + m] = v;
+        g.part_sum[(size_t)tile_n * g.M + m] = sum;
     }
 }
 
@@ -314,6 +314,7 @@ __global__ __launch_bounds__(256, 2) void gemm_i8_pair_kernel(GemmI8Group gg) {
         step(I0, at);
         if (at + 1 < steps) step(I1, at + 1);
     }
+    __builtin_amdgcn_s_waitcnt(0x0F70);      // vmcnt(0)
     __syncthreads();
 
     GemmBf16Params e = g;
@@ -343,13 +344,13 @@ hipError_t launch_gemm_i8(const GemmI8Group& g0, hipStream_t st) {
         if (r < g.n) g.total += (int)ceil_div(g.sh[r].rows, cols);
     }
     g.slices = 1;
-    auto few = [&](auto kernel, int rows, int waves) {
-        hipLaunchKernelGGL(kernel, dim3(g.total * (int)ceil_div(g.base.M, rows)), dim3(64 * waves), 0, st, g);
+    auto few = [&](auto kernel, int waves) {
+        hipLaunchKernelGGL(kernel, dim3(g.total), dim3(64 * waves), 0, st, g);
         return hipGetLastError();
     };
-    if (g.base.M <= 32) return few(gemm_i8_few_kernel<1, 4, 4>, 32, 4);
-    if (g.base.M <= 64) return few(gemm_i8_few_kernel<2, 4, 4>, 64, 4);
-    if (g.base.M <= FEW_MOST && g.base.K * 2 > PAIR_MOST_K) return few(gemm_i8_few_kernel<4, 8, 3>, 128, 8);
+    if (g.base.M <= 32) return few(gemm_i8_few_kernel<1, 4, 4>, 4);
+    if (g.base.M <= 64) return few(gemm_i8_few_kernel<2, 4, 4>, 4);
+    if (g.base.M <= FEW_MOST && g.base.K * 2 > PAIR_MOST_K) return few(gemm_i8_few_kernel<4, 8, 3>, 8);
     if (g.base.K * 2 > PAIR_MOST_K) return launch_fast_t<true, true, Epi::LogitsI8>(g, st);
     const int tiles = g.total * (int)ceil_div(g.base.M, PAIR_ROWS);
     bool stream = tiles > 2 * compute_unit_count();
