@@ -387,6 +387,7 @@ class OutputLayerI8Plan:
         H = norm.H if H is None else H
         if H.dim() != 2:
             raise B.VPError("H must be [N, h]")
+        W_shards = list(W_shards)
         self.H, self.norm = H, norm
         self.N, self.h = H.shape
         stride = B.vp_i8_row_stride(self.h)
@@ -438,6 +439,8 @@ class DraftVerifyPlan:
     def __init__(self, target, starts: torch.Tensor, drafts: torch.Tensor, uniforms: torch.Tensor, draft=None):
         if target.logits is None or (draft is not None and draft.logits is None):
             raise B.VPError("plans whose logits are drawn from keep them (save_logits)")
+        if starts.dim() != 1:
+            raise B.VPError("starts must be [sequences + 1]")
         self.target, self.draft = target, draft
         self.starts, self.drafts, self.uniforms = starts, drafts, uniforms
         self.logits, self.offsets = self._shards(target)

@@ -130,8 +130,12 @@ def test_refusals_of_the_plans():
     for a, k in (((alone,), {}), ((plan,), dict(draft=alone)), ((plan,), dict(draft=other))):
         with pytest.raises(vp.VPError):
             vp.DraftVerifyPlan(*a, starts, drafts, uniforms, **k)
+    for wrong in (starts[0], starts[:1], starts[:0]):
+        with pytest.raises(vp.VPError):
+            vp.DraftVerifyPlan(plan, wrong, drafts, uniforms)
     with pytest.raises(vp.VPError):
         vp.quantize_rows(torch.zeros(4, device="cuda"))
+    assert vp.OutputLayerI8Plan(H, iter(W)).vocab_size == 128
 
 
 def step_of(target, draft, verify):
