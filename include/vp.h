@@ -376,7 +376,8 @@ vp_status vp_grad_scale(const void* const* grads, const int64_t* counts, const i
  *     a_i = max_j |x_ij|,   scales[i] = a_i / 127,   q_ij = 127 x_ij / a_i rounded to the nearest integer, ties to even
  * The quotient is the exact one, so q does not depend on the order or width of any arithmetic.  A row of zeros has scale 0 and
  * q = 0; a row that holds an infinity or a NaN has scale NaN and q = 0 (its logits become NaN, other rows' do not).
- *   x [N,h] : in, type dt.   q [N, vp_i8_row_stride(h)] : out, int8, zero in the columns h and behind.   scales [N] : out, fp32.
+ *   x [N,h] : in, type dt.   q [N, vp_i8_row_stride(h)] : out, int8, zero in the columns h and behind.   scales [N] : out, fp32, at
+ *   any element.   No output shares memory with x or the other one.
  * vp_i8_row_stride: h rounded up to a multiple of 128 (-1 for h < 1 or h > 130944: sums of products stay below 2^31).
  */
 int64_t vp_i8_row_stride(int64_t h);
@@ -389,7 +390,8 @@ vp_status vp_quantize_rows(const void* x, int64_t N, int64_t h, vp_dtype dt, int
  * are zero (in one of the two at least).  logits_out (with VP_SAVE_LOGITS) is of type logits_dt.  A temperature is a factor of
  * H_scales.
  *   H [N,k], W_shard [Vs,k] : in, int8.  H_scales [N], W_scales [Vs] : in, fp32, finite and not negative (a NaN makes its row or
- *   column of the logits NaN), at any element.   Everything else as for vp_output_fwd.  No output shares memory with an input or another output.
+ *   column of the logits NaN).   Everything else as for vp_output_fwd; vectors may start at any element.  No output shares memory
+ *   with an input or another output.
  * The workspace has vp_output_i8_workspace_bytes(1, N, &Vs) bytes ((size_t)-1 for invalid arguments).
  *
  * vp_output_fwd_i8_group: p shards that live on one device, arguments as for vp_output_fwd_group (W_shards, W_scales and
@@ -418,8 +420,9 @@ vp_status vp_output_fwd_i8_group(const int8_t* H, const float* H_scales, const i
  * Where that sum is 0 (p nowhere above q: roundings of the statistics) it is drawn from p.  A row without a single possible
  * token (all logits -inf, or a NaN or +inf among them) gives the token -1.
  * Probabilities and sums are held in 64 bits, in a fixed order: results repeat bit for bit.
- *   logits, draft_logits : HOST arrays of p device pointers to [N, rows[r]], in, type dt, or NULL for draft_logits; they may start
- *   at any element.  -inf rules a token out.  The shards' ranges of the vocabulary do not overlap.
+ *   All tensors but the workspace may start at any element.
+ *   logits, draft_logits : HOST arrays of p device pointers to [N, rows[r]], in, type dt, or NULL for draft_logits.  -inf rules a
+ *   token out.  The shards' ranges of the vocabulary do not overlap.
  *   global_max, global_sumexp [N] : in, fp32, as vp_combine_stats leaves them.  draft_max, draft_sumexp [N] : in, or NULL.
  *   drafts [N] : in, int64; a draft that no shard owns is rejected, those of last rows are ignored.
  *   starts [sequences + 1] : in, int64, ascending, within [0, N] (values outside are taken as the nearest bound; a sequence
