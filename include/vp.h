@@ -392,7 +392,8 @@ vp_status vp_quantize_rows(const void* x, int64_t N, int64_t h, vp_dtype dt, int
  *   H [N,k], W_shard [Vs,k] : in, int8.  H_scales [N], W_scales [Vs] : in, fp32, finite and not negative (a NaN makes its row or
  *   column of the logits NaN).   Everything else as for vp_output_fwd; vectors may start at any element.  No output shares memory
  *   with an input or another output.
- * The workspace has vp_output_i8_workspace_bytes(1, N, &Vs) bytes ((size_t)-1 for invalid arguments).
+ * The workspace has vp_output_i8_workspace_bytes(1, N, &Vs) bytes ((size_t)-1 for invalid arguments), which suffice for fewer
+ * tokens too.
  *
  * vp_output_fwd_i8_group: p shards that live on one device, arguments as for vp_output_fwd_group (W_shards, W_scales and
  * logits_out HOST arrays of p device pointers), results those of p single calls.

@@ -1085,10 +1085,14 @@ size_t vp_output_i8_workspace_bytes(int32_t p, int64_t N, const int64_t* rows) {
     size_t need = 0;
     for (int32_t r0 = 0; r0 < p; r0 += GEMM_GROUP_MAX) {
         const int n = p - r0 < GEMM_GROUP_MAX ? p - r0 : GEMM_GROUP_MAX;
-        int64_t tiles = 0;
-        for (int k = 0; k < n; ++k) tiles += ceil_div(rows[r0 + k], gemm_i8_columns(N));
-        const size_t b = align_up((size_t)(2 * tiles + n) * N * sizeof(float), 256);
-        need = b > need ? b : need;
+        // for N tokens or fewer: of those with narrower tiles the most need the most
+        for (int64_t tokens = N < I8_NARROW_MOST ? N : I8_NARROW_MOST;; tokens = N) {
+            int64_t tiles = 0;
+            for (int k = 0; k < n; ++k) tiles += ceil_div(rows[r0 + k], gemm_i8_columns(tokens));
+            const size_t b = align_up((size_t)(2 * tiles + n) * tokens * sizeof(float), 256);
+            need = b > need ? b : need;
+            if (tokens == N) break;
+        }
     }
     return need;
 }

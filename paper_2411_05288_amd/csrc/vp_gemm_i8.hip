@@ -332,7 +332,7 @@ __global__ __launch_bounds__(256, 2) void gemm_i8_pair_kernel(GemmI8Group gg) {
 }  // namespace
 
 // Columns of a tile: a row of partial statistics each.
-int gemm_i8_columns(int64_t N) { return N <= 64 ? 128 : BN; }
+int gemm_i8_columns(int64_t N) { return N <= I8_NARROW_MOST ? 128 : BN; }
 
 hipError_t launch_gemm_i8(const GemmI8Group& g0, hipStream_t st) {
     ProfScope prof(K_GEMM_I8, st);
@@ -349,7 +349,7 @@ hipError_t launch_gemm_i8(const GemmI8Group& g0, hipStream_t st) {
         return hipGetLastError();
     };
     if (g.base.M <= 32) return few(gemm_i8_few_kernel<1, 4, 4>, 4);
-    if (g.base.M <= 64) return few(gemm_i8_few_kernel<2, 4, 4>, 4);
+    if (g.base.M <= I8_NARROW_MOST) return few(gemm_i8_few_kernel<2, 4, 4>, 4);
     if (g.base.M <= FEW_MOST && g.base.K * 2 > PAIR_MOST_K) return few(gemm_i8_few_kernel<4, 8, 3>, 8);
     if (g.base.K * 2 > PAIR_MOST_K) return launch_fast_t<true, true, Epi::LogitsI8>(g, st);
     const int tiles = g.total * (int)ceil_div(g.base.M, PAIR_ROWS);

@@ -277,7 +277,9 @@ struct GemmI8Group : GemmBf16Group {
     const float* col_scales[GEMM_GROUP_MAX];     // [rows]
     int out_f32;                                 // type of the logits that are kept: out of the shards is of this type
 };
-// Columns of a tile of N tokens: a row of partial statistics each (the launch fills first and total).
+// Columns of a tile of N tokens: a row of partial statistics each (the launch fills first and total).  Up to I8_NARROW_MOST tokens
+// have the narrower ones.
+constexpr int64_t I8_NARROW_MOST = 64;
 int gemm_i8_columns(int64_t N);
 hipError_t launch_gemm_i8(const GemmI8Group& g, hipStream_t st);
 

@@ -142,3 +142,12 @@ def test_verify_size_limits_and_workspace(lib):
     assert verify(lib, N=1 << 31) == UNSUPPORTED
     assert verify(lib, rows=[40, (1 << 20) + 1]) == UNSUPPORTED
     assert verify(lib, N=1 << 20, rows=[40, 1 << 11], wb=1 << 40) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("rows", [[1], [128], [129], [1000, 1], [4000] * 8, [16000] * 16, [300] * 17])
+def test_a_workspace_suffices_for_fewer_tokens(lib, rows):
+    """So one for the largest batch serves all of them, also where fewer tokens have narrower tiles."""
+    sizes = [lib.vp_output_i8_workspace_bytes(len(rows), N, array(ctypes.c_int64, rows)) for N in range(1, 300)]
+    assert sizes == sorted(sizes)
+    sizes = [lib.vp_verify_workspace_bytes(n, sum(rows)) for n in range(1, 300)]
+    assert sizes == sorted(sizes)
