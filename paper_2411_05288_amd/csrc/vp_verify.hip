@@ -65,11 +65,19 @@ __device__ __forceinline__ void fill_table(double* table) {
     if (threadIdx.x < TABLE) table[threadIdx.x] = exp2((double)threadIdx.x / TABLE);
     __syncthreads();
 }
+// `low` keeps the integer in its range (exp(-800) is 0; y = -inf would leave none).  From 2^28 on, fp32 numbers are 32 and more
+// apart, later thousands, and m - 800 would become m itself: the logits of such a row are shifted by m first (`close`), which is
+// exact where the difference counts.
 struct Exp {
-    float low;
+    float shift, low;
     double m, f;      // f exp(y - m)
-    // (exp(-800) is 0; y = -inf would leave no n)
-    __device__ Exp(float m, double f) : low(m - 800.f), m(m), f(f) {}
+    __device__ Exp(float top, double f) : shift(fabsf(top) >= 0x1p28f ? top : 0.f), low(top - shift - 800.f), m(top - shift), f(f) {}
+    template <typename T>
+    __device__ __forceinline__ void close(Raw<T>& y) const {
+        if (shift == 0.f) return;
+#pragma unroll
+        for (int e = 0; e < E; ++e) y.set(e, y[e] - shift);
+    }
     __device__ __forceinline__ double operator()(float y, const double* table) const {
         const double x = (double)__builtin_elementwise_maximum(y, low) - m;      // (a NaN stays one)
         constexpr double MAGIC = 6755399441055744.0;      // 1.5 2^52: a sum with it ends in the nearest integer
@@ -180,6 +188,8 @@ struct Weights {
         const size_t row = (size_t)at * s.rows;
         load8(y, (const T*)s.Y + row, j, s.rows);
         if (model) load8(z, (const T*)s.Z + row, j, s.rows);
+        p.close(y);
+        if (model) q.close(z);
     }
     __device__ __forceinline__ void get(double (&w)[E]) const {
 #pragma unroll

@@ -188,6 +188,54 @@ def test_statistics_without_a_number():
     assert t[0] == t[2] == t[4] == -1
 
 
+LARGE = [-1e30, "min", 3e38, 1e12, -2.0 ** 34, 2.0 ** 34, -2.0 ** 33, 2.0 ** 33, 2.0 ** 28, -2.0 ** 28, 2.0 ** 27, -2.0 ** 27]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("model", [True, False])
+@pytest.mark.parametrize("value", LARGE)
+def test_rows_of_large_logits(value, model, dtype):
+    """Rows whose largest logit has no number of its type within hundreds of it, as a constant far below all others leaves one where
+    it rules out every token but those of -inf: only the tokens that have it can be drawn, and none behind a shard's end."""
+    value = float(torch.finfo(TYPES[dtype]).min) if value == "min" else float(torch.tensor(value, dtype=TYPES[dtype]))
+    c = Case([0, 1, 2, 0, 3] * 8, [300, 77, 513], dtype, model, seed=21)
+    rng = np.random.default_rng(22)
+    lower = float(torch.tensor(value - abs(value) / 4, dtype=TYPES[dtype]))
+    for Y in (c.Y,) if c.Z is None else (c.Y, c.Z):
+        Y[:] = np.where(rng.random(Y.shape) < 0.5, -np.inf, lower)
+        Y[1::2] = -np.inf
+        has = rng.random(Y.shape) < np.repeat([0.5, 0.02], [300, 590])
+        has[np.arange(c.N), rng.integers(0, c.V, c.N)] = True      # (a token at least)
+        Y[has] = value
+    alone = c.starts[2]      # one token of the whole vocabulary, the last of the second shard
+    c.Y[alone] = -np.inf
+    c.Y[alone, 376] = value
+    c.uniforms[::7] = 0.0
+    c.stats()
+    accepted, t = c.run()
+    a, want, margins = c.want()
+    for i, token in enumerate(t):
+        assert token == -1 or (0 <= token < c.V and c.Y[i, token] == value)
+    np.testing.assert_array_equal(accepted, a)
+    assert (margins[c.uniforms[c.starts[1:] - 1] > 0] > 1e-12).all()      # (at 0 the first possible token is meant)
+    np.testing.assert_array_equal(t, want)
+
+
+@pytest.mark.parametrize("value", [v for v in LARGE if v not in (-1e30, "min", 3e38)])
+def test_neighbours_of_large_logits(value):
+    """Logits a few steps of their type below a large one keep their weights."""
+    c = Case([0, 1, 2, 3] * 10, [300, 77], "f32", seed=23)
+    rng = np.random.default_rng(24)
+    for Y in (c.Y, c.Z):
+        near = np.full(Y.shape, np.float32(value))
+        for k in range(1, 41):
+            step = np.nextafter(near, np.float32(-np.inf))
+            near = np.where(rng.random(Y.shape) < 0.9, step, near)
+        Y[:] = near
+    c.stats()
+    c.check()
+
+
 def test_nothing_is_left_of_the_difference():
     """p nowhere above q, as roundings of the statistics can leave it: the token is drawn from p."""
     c = Case([1] * 30, [3000, 2000], seed=10)
