@@ -410,6 +410,22 @@ vp_status vp_output_fwd_i8_group(const int8_t* H, const float* H_scales, const i
                                  void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Statistics of logits as they are stored: p shards (at most 64) that live on one device, the row maximum and the row sum of
+ * exponentials over all of them,
+ *     global_max[i] = max_j Y_ij,   global_sumexp[i] = sum_j exp(Y_ij - global_max[i])
+ * What vp_combine_stats leaves are those of the layer's values before they are rounded to bf16 and before the program changes them
+ * (rules tokens out with -inf, divides by a temperature): probabilities from stored logits that are to sum to 1 take these.
+ *   logits : HOST array of p device pointers to [N, rows[r]], in, type dt, at any element.   global_max, global_sumexp [N] : out,
+ *   fp32, at any element.  The maximum leaves a NaN out, the sum is NaN where there is one or a +inf; without any token but -inf
+ *   they are -inf and 0.  Sums are joined in 64 bits, in a fixed order.  No output shares memory with an input or another output.
+ * The workspace has vp_logits_stats_workspace_bytes(p, N, rows) bytes ((size_t)-1 for invalid arguments), which suffice for fewer
+ * rows too.
+ */
+size_t vp_logits_stats_workspace_bytes(int32_t p, int64_t N, const int64_t* rows);
+vp_status vp_logits_stats(const void* const* logits, const int64_t* rows, int32_t p, vp_dtype dt, int64_t N, float* global_max,
+                          float* global_sumexp, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Verification of drafted tokens against the logits of p shards (at most 64) that live on one device, and the draw of the token
  * behind them (speculative sampling).  Sequence b has the rows starts[b] .. starts[b+1] - 1 of the logits: one for each of its
  * drafts, drafts[i] the token that row i is asked about, and a last one without (a sequence of one row is plain sampling).
@@ -424,7 +440,9 @@ vp_status vp_output_fwd_i8_group(const int8_t* H, const float* H_scales, const i
  *   All tensors but the workspace may start at any element.
  *   logits, draft_logits : HOST arrays of p device pointers to [N, rows[r]], in, type dt, or NULL for draft_logits.  -inf rules a
  *   token out.  The shards' ranges of the vocabulary do not overlap.
- *   global_max, global_sumexp [N] : in, fp32, as vp_combine_stats leaves them.  draft_max, draft_sumexp [N] : in, or NULL.
+ *   global_max, global_sumexp [N] : in, fp32, the statistics of exactly these logits, as vp_logits_stats makes them.  With those of
+ *   other values p does not sum to 1, and tokens do not follow the target (vp_combine_stats' are of these values, up to roundings,
+ *   only where fp32 logits were kept and not changed since).  draft_max, draft_sumexp [N] : in, of draft_logits, or NULL.
  *   drafts [N] : in, int64; a draft that no shard owns is rejected, those of last rows are ignored.
  *   starts [sequences + 1] : in, int64, ascending, within [0, N] (values outside are taken as the nearest bound; a sequence
  *   without rows has 0 accepted and writes no tokens).   uniforms [N] : in, fp32, in [0, 1).

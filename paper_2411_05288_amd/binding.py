@@ -147,6 +147,10 @@ def load_library() -> ctypes.CDLL:
     lib.vp_output_fwd_i8.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i64, c.c_int, u32, vp, vp, vp, vp, vp, sz, vp]
     lib.vp_output_fwd_i8_group.restype = c.c_int
     lib.vp_output_fwd_i8_group.argtypes = [vp, vp, vp, vp, vp, vp, i32, vp, i64, i64, c.c_int, u32, vp, vp, vp, vp, vp, sz, vp]
+    lib.vp_logits_stats_workspace_bytes.restype = sz
+    lib.vp_logits_stats_workspace_bytes.argtypes = [i32, i64, vp]
+    lib.vp_logits_stats.restype = c.c_int
+    lib.vp_logits_stats.argtypes = [vp, vp, i32, c.c_int, i64, vp, vp, vp, sz, vp]
     lib.vp_verify_workspace_bytes.restype = sz
     lib.vp_verify_workspace_bytes.argtypes = [i32, i64]
     lib.vp_verify_drafts.restype = c.c_int
@@ -173,7 +177,8 @@ def load_library() -> ctypes.CDLL:
     lib.vp_profile_enable.argtypes = [c.c_int]
     lib.vp_profile_read.restype = c.c_int
     lib.vp_profile_read.argtypes = [c.POINTER(c.c_double), c.POINTER(c.c_int64), c.c_int]
-    for name in ("vp_block_norm_fwd", "vp_block_norm_bwd", "vp_quantize_rows", "vp_output_fwd_i8_group", "vp_verify_drafts"):
+    for name in ("vp_block_norm_fwd", "vp_block_norm_bwd", "vp_quantize_rows", "vp_output_fwd_i8_group", "vp_logits_stats",
+                 "vp_verify_drafts"):
         _ADDRESS[name] = c.cast(getattr(lib, name), vp).value
     _LIB, _HOST = lib, host      # (only now: the native checks call the library's functions)
     return lib
@@ -830,6 +835,35 @@ def vp_output_fwd_i8_group(H, H_scales, W_shards, W_scales, labels, shard_offset
     _check(st, "vp_output_fwd_i8_group")
 
 
+def vp_logits_stats_workspace_bytes(N: int, rows) -> int:
+    n = load_library().vp_logits_stats_workspace_bytes(len(rows), N, _i64s(rows))
+    if n == ctypes.c_size_t(-1).value:
+        raise VPError("vp_logits_stats_workspace_bytes: invalid arguments")
+    return n
+
+
+def vp_logits_stats(logits, global_max, global_sumexp, workspace, stream=None) -> None:
+    """Row maxima and row sums of exponentials [N] of the shards' logits ([N, rows] each) as they are stored: what
+    vp_verify_drafts takes."""
+    if isinstance(stream, torch.cuda.Stream):
+        stream = stream.cuda_stream
+    if _HOST is not None:
+        st = _HOST.logits_stats(_ADDRESS["vp_logits_stats"], logits, global_max, global_sumexp, workspace, stream)
+        if st is not None:      # the call was made
+            _check(st, "vp_logits_stats")
+            return
+    if not logits or any(t.dim() != 2 for t in logits):
+        raise VPError("logits must be [N, rows], a shard at least")
+    N, rows = logits[0].shape[0], [int(t.shape[1]) for t in logits]
+    f = (torch.float32,)
+    _on_current_device((*logits, global_max, global_sumexp, workspace))
+    wp, wb = _ws(workspace)
+    st = load_library().vp_logits_stats(
+        _each(logits, "logits", (logits[0].dtype,), [(N, n) for n in rows]), _i64s(rows), len(rows), _dtype_code(logits[0]), N,
+        _ptr(global_max, "global_max", f, (N,)), _ptr(global_sumexp, "global_sumexp", f, (N,)), wp, wb, _stream(stream))
+    _check(st, "vp_logits_stats")
+
+
 def vp_verify_workspace_bytes(sequences: int, V: int) -> int:
     n = load_library().vp_verify_workspace_bytes(sequences, V)
     if n == ctypes.c_size_t(-1).value:
@@ -839,8 +873,8 @@ def vp_verify_workspace_bytes(sequences: int, V: int) -> int:
 
 def vp_verify_drafts(logits, shard_offsets, global_max, global_sumexp, drafts, starts, uniforms, accepted, tokens, workspace, *,
                      draft_logits=None, draft_max=None, draft_sumexp=None, stream=None) -> None:
-    """Verification of drafted tokens over the shards' logits ([N, rows] each) and the draw of the token behind them.  Sequence b
-    has the rows starts[b] .. starts[b + 1] - 1, one for each draft and a last one; draft_*: the draft model's, row by row, or
+    """Verification of drafted tokens over the shards' logits ([N, rows] each) and the draw of the token behind them.  The
+    statistics are those of exactly these logits (vp_logits_stats).  Sequence b has the rows starts[b] .. starts[b + 1] - 1, one for each draft and a last one; draft_*: the draft model's, row by row, or
     None (drafts that no model drew).  accepted [sequences] int32, tokens [N]: accepted drafts, the next token, -1 behind it."""
     if isinstance(stream, torch.cuda.Stream):
         stream = stream.cuda_stream

@@ -1178,6 +1178,37 @@ vp_status vp_output_fwd_i8(const int8_t* H, const float* H_scales, const int8_t*
                                   workspace_bytes, stream);
 }
 
+// ---- statistics of stored logits
+
+size_t vp_logits_stats_workspace_bytes(int32_t p, int64_t N, const int64_t* rows) {
+    if (p < 1 || p > VERIFY_MAX_SHARDS || !rows || N < 1) return (size_t)-1;
+    for (int32_t r = 0; r < p; ++r)
+        if (rows[r] < 1 || !sizes_supported(N, 1, rows[r])) return (size_t)-1;
+    return logits_stats_workspace(p, N, rows);
+}
+
+vp_status vp_logits_stats(const void* const* logits, const int64_t* rows, int32_t p, vp_dtype dt, int64_t N, float* global_max,
+                          float* global_sumexp, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!logits || !rows || p < 1 || !dtype_ok(dt) || N < 1 || !global_max || !global_sumexp) return VP_ERR_INVALID_ARG;
+    if ((((uintptr_t)global_max | (uintptr_t)global_sumexp) & 3u) || !aligned16(workspace)) return VP_ERR_INVALID_ARG;
+    if (p > VERIFY_MAX_SHARDS || N >= MAX_ELEMS) return VP_ERR_UNSUPPORTED;
+    for (int32_t r = 0; r < p; ++r) {
+        if (!logits[r] || ((uintptr_t)logits[r] & (elem_bytes(dt) - 1)) || rows[r] < 1) return VP_ERR_INVALID_ARG;
+        if (!sizes_supported(N, 1, rows[r])) return VP_ERR_UNSUPPORTED;
+    }
+    const size_t need = vp_logits_stats_workspace_bytes(p, N, rows);
+    if (!workspace || workspace_bytes < need) return VP_ERR_WORKSPACE;
+    const Output m{global_max, (size_t)N * 4}, s{global_sumexp, (size_t)N * 4}, w{workspace, need};
+    Verify v{};
+    for (int32_t r = 0; r < p; ++r) {
+        if (!outputs_apart({{logits[r], (size_t)N * rows[r] * elem_bytes(dt)}}, {m, s, w})) return VP_ERR_INVALID_ARG;
+        v.sh[r] = {logits[r], nullptr, 0, (int)rows[r], 0};
+    }
+    v.p = p;
+    v.N = N;
+    return dev(launch_logits_stats(v, dt, global_max, global_sumexp, workspace, (hipStream_t)stream));
+}
+
 // ---- verification of drafts
 
 constexpr int32_t MAX_SEQUENCES = 1 << 23;      // a workgroup each at least: a launch has fewer than 2^32 threads

@@ -425,6 +425,37 @@ PyObject* output_fwd_i8_group(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return PyLong_FromLong(status);
 }
 
+using LogitsStats = int (*)(const void* const*, const int64_t*, int32_t, int, int64_t, void*, void*, void*, size_t, void*);
+
+// logits_stats(function, logits, global_max, global_sumexp, workspace, stream) -> status
+PyObject* logits_stats(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 6) Py_RETURN_NONE;
+    int status = 0;
+    try {
+        Call c;
+        const auto f = reinterpret_cast<LogitsStats>(c.pointer(a[0]));
+        int64_t rows[MOST];
+        const void* Y[MOST];
+        const int p = c.sizes(a[1], 1, 2, rows, MOST);
+        if (!c.ok) Py_RETURN_NONE;
+        const int64_t N = THPVariable_Unpack(PyList_GET_ITEM(a[1], 0)).size(0);
+        const at::ScalarType type = c.type_of(a[1]);
+        const int dt = vp_dtype_of(type);
+        if (dt < 0) Py_RETURN_NONE;
+        c.each(a[1], p, type, rows, N, Call::Columns, Y);
+        void *m = c.at(a[2], 0, {N}), *s = c.at(a[3], 0, {N});
+        size_t bytes = 0;
+        void *workspace = c.memory(a[4], bytes), *stream = c.stream(a[5]);
+        if (!c.ok) Py_RETURN_NONE;
+        Py_BEGIN_ALLOW_THREADS
+        status = f(Y, rows, p, dt, N, m, s, workspace, bytes, stream);
+        Py_END_ALLOW_THREADS
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    return PyLong_FromLong(status);
+}
+
 // verify_drafts(function, logits, shard_offsets, global_max, global_sumexp, drafts, starts, uniforms, accepted, tokens, workspace,
 //               draft_logits, draft_max, draft_sumexp, stream) -> status
 PyObject* verify_drafts(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -464,6 +495,7 @@ PyObject* verify_drafts(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyMethodDef methods[] = {
     {"quantize_rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(quantize_rows)), METH_FASTCALL, nullptr},
     {"output_fwd_i8_group", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(output_fwd_i8_group)), METH_FASTCALL, nullptr},
+    {"logits_stats", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(logits_stats)), METH_FASTCALL, nullptr},
     {"verify_drafts", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(verify_drafts)), METH_FASTCALL, nullptr},
     {"block_norm_fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(block_norm_fwd)), METH_FASTCALL, nullptr},
     {"block_norm_bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(block_norm_bwd)), METH_FASTCALL, nullptr},

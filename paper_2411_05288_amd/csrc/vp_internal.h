@@ -19,7 +19,7 @@ static inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; 
 enum KernelId : int {
     K_GEMM_FWD_STATS = 0, K_GEMM_DLOGITS, K_GEMM_DH, K_GEMM_DW, K_FOLD, K_COMBINE, K_DLOGITS_EW, K_GEMM_F32,
     K_ROWSTATS_F32, K_EMBED_FWD, K_EMBED_SORT, K_EMBED_ACCUM, K_GEMM_A_ALG2, K_DX_ALG2, K_SUM_SLICES, K_ZERO_PAD,
-    K_BLOCK_NORM_FWD, K_BLOCK_NORM_BWD, K_GRAD_NORM, K_GRAD_SCALE, K_QUANTIZE, K_GEMM_I8, K_VERIFY, K_COUNT
+    K_BLOCK_NORM_FWD, K_BLOCK_NORM_BWD, K_GRAD_NORM, K_GRAD_SCALE, K_QUANTIZE, K_GEMM_I8, K_VERIFY, K_LOGITS_STATS, K_COUNT
 };
 
 // Brackets the launches made during its lifetime with two events when timing is enabled;
@@ -302,5 +302,9 @@ struct Verify {
 };
 size_t verify_workspace(int64_t sequences, int64_t V);
 hipError_t launch_verify(const Verify& v, vp_dtype dt, void* workspace, hipStream_t st);
+
+// Statistics of stored logits (Y, rows, p and N of `v`).
+size_t logits_stats_workspace(int32_t p, int64_t N, const int64_t* rows);
+hipError_t launch_logits_stats(const Verify& v, vp_dtype dt, float* gmax, float* gsum, void* workspace, hipStream_t st);
 
 }  // namespace vp

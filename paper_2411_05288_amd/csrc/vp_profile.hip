@@ -50,7 +50,7 @@ static const char* const kNames[K_COUNT] = {
     "combine_stats", "dlogits_elementwise", "gemm_f32", "row_stats_f32", "embed_fwd",
     "embed_bwd_sort", "embed_bwd_accum", "gemm_bf16_A_alg2", "dx_alg2",
     "sum_slices", "zero_pad_columns",
-    "block_norm_fwd", "block_norm_bwd", "grad_norm", "grad_scale", "quantize_rows", "gemm_i8_fwd_stats", "verify_drafts"};
+    "block_norm_fwd", "block_norm_bwd", "grad_norm", "grad_scale", "quantize_rows", "gemm_i8_fwd_stats", "verify_drafts", "logits_stats"};
 
 }  // namespace vp
 

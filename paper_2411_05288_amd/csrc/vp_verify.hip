@@ -1,4 +1,5 @@
-// Verification of drafted tokens over the shards' logits and the draw of the next token (vp.h has the formulas).
+// Verification of drafted tokens over the shards' logits and the draw of the next token, and the statistics of stored logits that
+// it takes (vp.h has the formulas).
 //
 // Two launches: the sums of the weights of every segment of 512 tokens of the row that the next token is drawn from, then the
 // search for the segment and the token in it.  Which row that is, every wavefront of the first launch finds out by itself: a draft
@@ -401,7 +402,110 @@ __global__ __launch_bounds__(THREADS) void verify_pick_kernel(Verify v, int segm
         v.tokens[i] = i < f.at ? v.drafts[i] : i == f.at ? token : -1;
 }
 
+// ---- statistics of stored logits: a wavefront for every CHUNK columns of a row, then one for every row, which joins them.
+//
+// Bound by reading the logits: 1276 rows of V=256000 bf16 128 us (5.1 TB/s), 226 of V=128256 14.8, 64 of V=128256 fp32 11.2; a few
+// rows by the two launches (5 of V=32000: 9.0).
+constexpr int SETS = 4, CHUNK = SETS * SEGMENT;
+
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
+    return x;
+}
+template <typename X>
+__device__ __forceinline__ X wave_sum(X x) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+    return x;
+}
+// What exponents are taken around: 0 where there is no number, so that -inf adds nothing and a NaN stays one.
+__device__ __forceinline__ float around(float m) { return m == -INFINITY ? 0.f : m; }
+
+// The columns stay in registers between the maximum and the sum, so they are read once.  Exponentials are of 32 bits: a term is off
+// by its distance from the maximum times 2^-23, which its size outweighs.
+template <typename T>
+__global__ __launch_bounds__(THREADS) void logits_stats_kernel(Verify v, int chunks, float2* __restrict__ part) {
+    const Lanes shards(v);
+    const int c = blockIdx.y * (blockDim.x >> 6) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (c >= chunks) return;
+    const VerifyShard& s = v.sh[shards.shard_of(c)];
+    const int j = (c - s.first) * CHUNK + (threadIdx.x & 63) * E;
+    for (int64_t i = blockIdx.x; i < v.N; i += gridDim.x) {
+        Raw<T> y[SETS];
+#pragma unroll
+        for (int k = 0; k < SETS; ++k) load8(y[k], (const T*)s.Y + (size_t)i * s.rows, j + k * SEGMENT, s.rows);
+        float m = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < SETS; ++k)
+#pragma unroll
+            for (int e = 0; e < E; ++e) m = fmaxf(m, y[k][e]);
+        m = wave_max(m);
+        const float a = around(m);
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < SETS; ++k) {
+            float x[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = __builtin_amdgcn_exp2f((y[k][e] - a) * 1.44269504088896340736f);
+            sum += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+        }
+        sum = wave_sum(sum);
+        if ((threadIdx.x & 63) == 0) part[(size_t)i * chunks + c] = make_float2(m, sum);
+    }
+}
+
+__global__ __launch_bounds__(THREADS) void join_stats_kernel(const float2* __restrict__ part, int chunks, int64_t N, float* __restrict__ gmax,
+                                                             float* __restrict__ gsum) {
+    for (int64_t i = (int64_t)blockIdx.x * WAVES + (threadIdx.x >> 6); i < N; i += (int64_t)gridDim.x * WAVES) {
+        float m = -INFINITY;
+        double sum = 0.0;
+        for (int c = threadIdx.x & 63; c < chunks; c += 64) {
+            const float2 q = part[(size_t)i * chunks + c];
+            const float top = fmaxf(m, q.x);
+            const double a = around(top);
+            sum = sum * exp(m - a) + q.y * exp(q.x - a);
+            m = top;
+        }
+        const float top = wave_max(m);
+        sum = wave_sum(sum * exp(m - (double)around(top)));
+        if ((threadIdx.x & 63) == 0) {
+            gmax[i] = top;
+            gsum[i] = (float)sum;
+        }
+    }
+}
+
 }  // namespace
+
+static int64_t stats_chunks(int32_t p, const int64_t* rows) {
+    int64_t n = 0;
+    for (int32_t r = 0; r < p; ++r) n += ceil_div(rows[r], CHUNK);
+    return n;
+}
+size_t logits_stats_workspace(int32_t p, int64_t N, const int64_t* rows) {
+    return align_up((size_t)(N * stats_chunks(p, rows)) * sizeof(float2), 256);
+}
+
+hipError_t launch_logits_stats(const Verify& v0, vp_dtype dt, float* gmax, float* gsum, void* workspace, hipStream_t st) {
+    ProfScope prof(K_LOGITS_STATS, st);
+    Verify v = v0;
+    int chunks = 0;
+    for (int r = 0; r < v.p; ++r) {
+        v.sh[r].first = chunks;
+        chunks += (int)ceil_div(v.sh[r].rows, CHUNK);
+    }
+    // a workgroup for every row where a launch has fewer than 2^31 threads then
+    const int waves = chunks < WAVES ? chunks : WAVES;
+    const int64_t groups = ceil_div(chunks, waves), most = ((int64_t)1 << 23) / groups;
+    const dim3 grid((unsigned)(v.N < most ? v.N : most), (unsigned)groups);
+    float2* part = (float2*)workspace;
+    if (dt == VP_F32) hipLaunchKernelGGL(logits_stats_kernel<float>, grid, dim3(64 * waves), 0, st, v, chunks, part);
+    else hipLaunchKernelGGL(logits_stats_kernel<u16>, grid, dim3(64 * waves), 0, st, v, chunks, part);
+    const int64_t joins = ceil_div(v.N, WAVES);
+    hipLaunchKernelGGL(join_stats_kernel, dim3((unsigned)(joins < 65536 ? joins : 65536)), dim3(THREADS), 0, st, part, chunks, v.N, gmax, gsum);
+    return hipGetLastError();
+}
 
 // The segments' sums, and the rows found.
 size_t verify_workspace(int64_t sequences, int64_t V) {

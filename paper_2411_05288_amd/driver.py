@@ -429,39 +429,62 @@ class OutputLayerI8Plan:
                            self.loss_rows, self.loss, stream)
 
 
+class KeptLogits:
+    """The logits that a plan keeps, as DraftVerifyPlan reads them, and their statistics ``global_max`` and ``global_sumexp``: those
+    of exactly the values that are stored.  (The plan's own are taken before the logits are rounded to bf16, and before the program
+    changes them.)  Whatever else is asked for is the plan's."""
+
+    def __init__(self, plan):
+        if plan.logits is None:
+            raise B.VPError("plans whose logits are drawn from keep them (save_logits)")
+        live = [r for r, v in enumerate(plan.valid) if v > 0]
+        self.plan = plan
+        self.logits, self.offsets = [plan.logits[r] for r in live], [plan.offsets[r] for r in live]
+        rows = [int(t.shape[1]) for t in self.logits]
+        self.global_max, self.global_sumexp = (torch.empty((plan.N,), dtype=torch.float32, device=self.logits[0].device)
+                                               for _ in range(2))
+        self.workspace = torch.empty((B.vp_logits_stats_workspace_bytes(plan.N, rows),), dtype=torch.uint8,
+                                     device=self.logits[0].device)
+
+    def __getattr__(self, name):
+        if name == "plan":      # (not made yet)
+            raise AttributeError(name)
+        return getattr(self.plan, name)
+
+    def statistics(self, stream=None) -> None:
+        B.vp_logits_stats(self.logits, self.global_max, self.global_sumexp, self.workspace, stream)
+
+
 class DraftVerifyPlan:
     """Verification of drafted tokens against the logits that ``target`` keeps (an OutputLayerPlan or OutputLayerI8Plan), and the
     draw of the token behind them.  Sequence b has the rows starts[b] .. starts[b + 1] - 1 of the target's tokens, one for each
     of its drafts and a last one; ``drafts`` [N] holds the token that each row is asked about, ``uniforms`` [N] random numbers in
-    [0, 1).  ``draft``: the plan of the model that drew the drafts, with the same shards and rows (its last rows are not read),
-    or None.  Results: ``accepted`` [sequences], ``tokens`` [N]."""
+    [0, 1).  ``draft``: the plan of the model that drew the drafts, with the same shards and rows (its last rows stand for
+    nothing), or None.  Tokens follow softmax of the logits as they are stored when ``forward`` is called: before it a program
+    may rule tokens out in them (-inf) or divide them by a temperature.  Results: ``accepted`` [sequences], ``tokens`` [N]."""
 
     def __init__(self, target, starts: torch.Tensor, drafts: torch.Tensor, uniforms: torch.Tensor, draft=None):
-        if target.logits is None or (draft is not None and draft.logits is None):
-            raise B.VPError("plans whose logits are drawn from keep them (save_logits)")
         if starts.dim() != 1:
             raise B.VPError("starts must be [sequences + 1]")
-        self.target, self.draft = target, draft
+        self.target, self.draft = KeptLogits(target), None if draft is None else KeptLogits(draft)
         self.starts, self.drafts, self.uniforms = starts, drafts, uniforms
-        self.logits, self.offsets = self._shards(target)
+        self.logits, self.offsets = self.target.logits, self.target.offsets
         self.draft_logits = None
         if draft is not None:
-            self.draft_logits, offsets = self._shards(draft)
-            if offsets != self.offsets or [t.shape for t in self.logits] != [t.shape for t in self.draft_logits]:
+            self.draft_logits = self.draft.logits
+            if self.draft.offsets != self.offsets or [t.shape for t in self.logits] != [t.shape for t in self.draft_logits]:
                 raise B.VPError("the plans of the target and of the draft model have the same shards and rows")
         V, sequences = sum(int(t.shape[1]) for t in self.logits), starts.shape[0] - 1
         self.accepted = torch.empty((max(sequences, 0),), dtype=torch.int32, device=starts.device)
         self.tokens = torch.empty((target.N,), dtype=torch.int64, device=starts.device)
         self.workspace = torch.empty((B.vp_verify_workspace_bytes(sequences, V),), dtype=torch.uint8, device=starts.device)
 
-    @staticmethod
-    def _shards(plan):
-        live = [r for r, v in enumerate(plan.valid) if v > 0]
-        return [plan.logits[r] for r in live], [plan.offsets[r] for r in live]
-
     def forward(self, stream=None) -> None:
-        d = self.draft
-        B.vp_verify_drafts(self.logits, self.offsets, self.target.global_max, self.target.global_sumexp, self.drafts, self.starts,
+        t, d = self.target, self.draft
+        t.statistics(stream)
+        if d is not None:
+            d.statistics(stream)
+        B.vp_verify_drafts(self.logits, self.offsets, t.global_max, t.global_sumexp, self.drafts, self.starts,
                            self.uniforms, self.accepted, self.tokens, self.workspace, draft_logits=self.draft_logits,
                            draft_max=None if d is None else d.global_max, draft_sumexp=None if d is None else d.global_sumexp,
                            stream=stream)

@@ -151,3 +151,37 @@ def test_a_workspace_suffices_for_fewer_tokens(lib, rows):
     assert sizes == sorted(sizes)
     sizes = [lib.vp_verify_workspace_bytes(n, sum(rows)) for n in range(1, 300)]
     assert sizes == sorted(sizes)
+
+
+# ------------------------------------------------------------------------------------------------ vp_logits_stats
+def statistics(lib, **k):
+    a = dict(Y=[P[0], P[1]], rows=[40, 30], p=2, dt=1, N=8, m=P[2], s=P[3], ws=P[4], wb=MB)
+    a.update(k)
+    a["Y"], a["rows"] = array(ctypes.c_void_p, a["Y"]), array(ctypes.c_int64, a["rows"])
+    return lib.vp_logits_stats(*a.values(), None)
+
+
+@pytest.mark.parametrize("wrong", [
+    *[{n: None} for n in ("Y", "rows", "m", "s")], dict(p=0), dict(p=-1), dict(dt=2), dict(N=0), dict(N=-1), dict(Y=[P[0], None]),
+    dict(rows=[0, 30]), dict(rows=[40, -1]), dict(Y=[P[0] + 1, P[1]]), dict(dt=0, Y=[P[0], P[1] + 2]), dict(m=P[2] + 2), dict(s=P[3] + 1),
+    dict(ws=P[4] + 8), dict(m=P[3]), dict(s=P[2] + 28), dict(m=P[4]), dict(s=P[0] + 636), dict(m=P[1]), dict(ws=P[1])])
+def test_statistics_refuse(lib, wrong):
+    assert statistics(lib, **wrong) == INVALID
+
+
+def test_statistics_size_limits_and_workspace(lib):
+    size = lambda p, N, rows: lib.vp_logits_stats_workspace_bytes(p, N, array(ctypes.c_int64, rows))      # noqa: E731
+    need = size(2, 8, [40, 30])
+    assert 0 < need < BAD
+    assert statistics(lib, wb=need - 1) == WORKSPACE and statistics(lib, ws=None) == WORKSPACE
+    assert statistics(lib, p=65, Y=[P[0]] * 65, rows=[1] * 65) == UNSUPPORTED
+    assert statistics(lib, N=1 << 31) == UNSUPPORTED
+    assert statistics(lib, rows=[40, (1 << 20) + 1]) == UNSUPPORTED
+    assert statistics(lib, N=1 << 20, rows=[40, 1 << 11], wb=1 << 40) == UNSUPPORTED
+    for wrong in ((0, 8, [40]), (65, 8, [40] * 65), (1, 0, [40]), (1, -1, [40]), (1, 8, [0]), (2, 8, [40, -1]), (1, 8, [(1 << 20) + 1]),
+                  (1, 1 << 31, [1])):
+        assert size(*wrong) == BAD
+    assert lib.vp_logits_stats_workspace_bytes(1, 8, None) == BAD
+    for rows in ([1], [2048], [2049, 1], [16000] * 16, [300] * 17):
+        sizes = [size(len(rows), N, rows) for N in range(1, 300)]
+        assert sizes == sorted(sizes)

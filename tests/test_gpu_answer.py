@@ -209,3 +209,103 @@ def test_rows_become_integers_on_another_stream():
     stream.synchronize()
     for t in (b, c):
         assert torch.equal(a[0], t[0]) and torch.equal(a[1], t[1])
+
+
+def sum_bound(Y, m):
+    """Bound of the relative error of fp32 sums of exp(y - m) over the rows of Y.  The difference d, its product with log2(e), that
+    constant and the exponential are off by 2^-24 (half a step) of d, d, 0.23 d and 2 steps of the term: 2.3 d 2^-24 + 2^-22.  Sums: 16
+    roundings one after the other at most, and the last one."""
+    with np.errstate(invalid="ignore"):
+        d = np.where(Y == -np.inf, 0.0, m[:, None] - Y)
+        w = np.where(Y == -np.inf, 0.0, np.exp(Y - m[:, None]))
+    return ((w * (2.3 * d + 4)).sum(1) / w.sum(1) + 17) * 2.0 ** -24
+
+
+def check_normalised(verify):
+    """What the verification calls probabilities are, as softmax of the logits that it reads: their sums are 1."""
+    for side, logits in ((verify.target, verify.logits), (verify.draft, verify.draft_logits)):
+        if side is not None:
+            Y = torch.cat([y.double() for y in logits], 1).cpu().numpy()
+            m, s = (t.double().cpu().numpy() for t in (side.global_max, side.global_sumexp))
+            total = np.exp(Y - m[:, None]).sum(1) / s
+            assert (np.abs(total - 1) <= 1.01 * sum_bound(Y, m)).all()
+
+
+class Peaked:
+    """A plan whose rows all are the same, with leading logits of this size."""
+
+    def __init__(self, kind, N, rows, seed, size, dtype=torch.bfloat16):
+        import paper_2411_05288_amd as vp
+        h, W = 128, weights(rows, 128, seed)
+        x = torch.randn(h, generator=torch.Generator(device="cuda").manual_seed(seed + 50), device="cuda")
+        x = x * (size / (torch.cat(W).float() @ x).max())
+        H = x.to(dtype).expand(N, h).contiguous()
+        if kind == "i8":
+            self.plan = vp.OutputLayerI8Plan(H, [vp.quantize_rows(w) for w in W])
+        else:
+            self.plan = vp.OutputLayerPlan(H, [w.to(dtype) for w in W], torch.zeros(N, dtype=torch.int64, device="cuda"), algorithm=kind)
+
+    def probabilities(self):
+        Y = torch.cat([y[0].double() for y in self.plan.logits]).cpu().numpy()
+        return np.exp(Y - Y.max()) / np.exp(Y - Y.max()).sum()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("size", [3.0, 20.0, 40.0])
+@pytest.mark.parametrize("kind", ["i8", 1, 2])
+def test_statistics_are_those_of_the_kept_logits(kind, size, dtype):
+    """The layers' own statistics are taken before the logits are rounded to bf16."""
+    import paper_2411_05288_amd as vp
+    counts, rows = [3, 0, 2, 8, 1], [200, 133, 300]
+    starts, drafts, uniforms = inputs(counts, sum(rows), 5)
+    target, draft = (Peaked(kind, int(starts[-1]), rows, s, size, dtype) for s in (1, 2))
+    verify = vp.DraftVerifyPlan(target.plan, starts, drafts, uniforms, draft=draft.plan)
+    for model in (draft, target):
+        model.plan.forward()
+    own = [(p.global_max.clone(), p.global_sumexp.clone(), p.loss_rows.clone()) for p in (target.plan, draft.plan)]
+    verify.forward()
+    check_normalised(verify)
+    check(verify, np.arange(sum(rows)))
+    for p, kept in zip((target.plan, draft.plan), own):      # (what a backward pass or the loss takes stays)
+        assert all(torch.equal(a, b) for a, b in zip((p.global_max, p.global_sumexp, p.loss_rows), kept))
+
+
+@pytest.mark.parametrize("model", [True, False])
+@pytest.mark.parametrize("change", ["none", "mask", "mask_low", "temperature"])
+@pytest.mark.parametrize("kind", ["i8", 1])
+def test_tokens_follow_the_kept_logits(kind, change, model):
+    """Whatever the drafts are, the first token of a sequence is distributed as softmax of the target's kept logits says, also where
+    the program rules tokens out (with -inf, or a constant far below) or divides by a temperature.  Of S sequences a token's count
+    is within 6 deviations and 12 of S p (Bernstein's inequality: below 2e-8 for a token; the seeds are fixed)."""
+    import paper_2411_05288_amd as vp
+    S, rows = 10000, [100, 57]
+    V, N = sum(rows), 2 * S
+    target, draft = (Peaked(kind, N, rows, s, 20.0) for s in (1, 2))
+    rng = np.random.default_rng(7)
+    for m in (target, draft):
+        m.plan.forward()
+    top = int(target.probabilities().argmax())
+    for y, at in zip(target.plan.logits, target.plan.offsets):
+        if change.startswith("mask"):
+            out = [j - at for j in {top, *range(0, V, 3)} if 0 <= j - at < y.shape[1]]
+            y[:, out] = -np.inf if change == "mask" else -1e30
+        elif change == "temperature":
+            y.div_(0.7)
+    p, q = target.probabilities(), draft.probabilities()
+    if model:
+        drawn = rng.choice(V, N, p=q)
+    else:
+        drawn = np.full(N, int(p.argmax()))
+    verify = vp.DraftVerifyPlan(target.plan, torch.arange(0, N + 1, 2, device="cuda"), torch.from_numpy(drawn).cuda(),
+                                torch.from_numpy(rng.random(N).astype(np.float32)).cuda(), draft=draft.plan if model else None)
+    verify.forward()
+    torch.cuda.synchronize()
+    check_normalised(verify)
+    within = lambda n, S, p: (np.abs(n - S * p) <= 6 * np.sqrt(S * p * (1 - p)) + 12).all()      # noqa: E731
+    first = np.bincount(verify.tokens[0::2].cpu().numpy(), minlength=V)
+    assert within(first, S, p) and not first[p == 0].any()
+    accepted = verify.accepted.cpu().numpy()
+    assert within(accepted.sum(), S, np.minimum(p, q).sum() if model else p.max())
+    behind = verify.tokens[1::2].cpu().numpy()[accepted == 1]
+    assert within(np.bincount(behind, minlength=V), len(behind), p)
+    assert (verify.tokens[1::2].cpu().numpy()[accepted == 0] == -1).all()
