@@ -390,8 +390,9 @@ vp_status vp_quantize_rows(const void* x, int64_t N, int64_t h, vp_dtype dt, int
  * are zero (in one of the two at least).  logits_out (with VP_SAVE_LOGITS) is of type logits_dt.  A temperature is a factor of
  * H_scales.
  *   H [N,k], W_shard [Vs,k] : in, int8.  H_scales [N], W_scales [Vs] : in, fp32, finite and not negative (a NaN makes its row or
- *   column of the logits NaN).   Everything else as for vp_output_fwd; vectors may start at any element.  No output shares memory
- *   with an input or another output.
+ *   column of the logits NaN, and the sums of exponentials that these are part of; maxima are those of the other logits, and if
+ *   there are none no number that stands for anything).  Everything else as for vp_output_fwd; vectors may start at any element.
+ *   No output shares memory with an input or another output.
  * The workspace has vp_output_i8_workspace_bytes(1, N, &Vs) bytes ((size_t)-1 for invalid arguments), which suffice for fewer
  * tokens too.
  *

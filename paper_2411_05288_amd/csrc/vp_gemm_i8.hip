@@ -168,9 +168,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group 
             v = fmaxf(v, y[r]);
         }
         v = fmaxf(v, __shfl_xor(v, 32, 64));
+        const float around = v == -INFINITY ? NO_MAX : v;
         float sum = 0.f;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sum += exp2_fast((y[r] - v) * LOG2E);
+        for (int r = 0; r < 16; ++r) sum += exp2_fast((y[r] - around) * LOG2E);
         sum += __shfl_xor(sum, 32, 64);
         if (hf == 0) {
             xm[wave][m] = v;
@@ -214,9 +215,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group 
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) v = fmaxf(v, xm[w][m]);
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w)
-            if (xm[w][m] > -INFINITY) sum += xs[w][m] * __expf(xm[w][m] - v);
-        g.part_max[(size_t)tile_n * g.M + m] = v;
+        for (int w = 0; w < WAVES; ++w) sum += part_sum_i8(xm[w][m], xs[w][m], v);
+        g.part_max[(size_t)tile_n * g.M + m] = part_max_i8(v, sum);
         g.part_sum[(size_t)tile_n * g.M + m] = sum;
     }
 }

@@ -24,6 +24,14 @@ struct I8Inputs {
     }
 };
 
+// Sums around a maximum: a NaN among the logits makes them NaN, also where a maximum, which leaves NaN out, has nothing else.  The
+// exponents are then taken around NO_MAX, so a sum over nothing but columns past the end is 0 and one with a NaN is NaN.
+constexpr float NO_MAX = -1e38f;
+// What a wavefront's sum adds to the tile's, whose maximum is m.
+__device__ __forceinline__ float part_sum_i8(float own, float sum, float m) { return own > -INFINITY ? sum * __expf(own - m) : sum; }
+// The tile's maximum as it is stored: the fold leaves out sums around -inf, which those that are NaN must not be.
+__device__ __forceinline__ float part_max_i8(float m, float sum) { return sum != sum ? fmaxf(m, -3.402823466e38f) : m; }
+
 // Wavefront-private staging block -> global memory, fp32 (see flush_stage_bf16).
 template <typename St, bool STREAM>
 __device__ __forceinline__ void flush_stage_f32(const char* region, __amdgpu_buffer_rsrc_t rs, unsigned off, unsigned row_bytes,
@@ -130,8 +138,8 @@ __device__ __forceinline__ void gemm_epilogue_i8(floatx16 (&acc)[MI][4], const G
 #pragma unroll
                 for (int r = 0; r < 16; ++r) v = fmaxf(v, acc[i][j][r]);
             v = fmaxf(v, __shfl_xor(v, 32, 64));
-            // (a wavefront whose columns all lie past the shard has -inf here; its sum is never used)
-            const float c = scale * LOG2E, vc = v * c;
+            // (-inf: no column but past the shard's end, which add 0, or NaN)
+            const float c = scale * LOG2E, vc = (v == -INFINITY ? NO_MAX : v) * c;
             // (eight exponentials at a time: each has to be waited for)
             float part[8] = {};
 #pragma unroll
@@ -194,10 +202,8 @@ __device__ __forceinline__ void gemm_epilogue_i8(floatx16 (&acc)[MI][4], const G
     __syncthreads();
     if (tid < TM && m0 + tid < g.M) {
         const float a = xm[tid], b = xm[256 + tid], m = fmaxf(a, b);
-        float s = 0.f;
-        if (a > -INFINITY) s += xs[tid] * __expf(a - m);
-        if (b > -INFINITY) s += xs[256 + tid] * __expf(b - m);
-        g.part_max[(size_t)tile_n * g.M + m0 + tid] = m;
+        const float s = part_sum_i8(a, xs[tid], m) + part_sum_i8(b, xs[256 + tid], m);
+        g.part_max[(size_t)tile_n * g.M + m0 + tid] = part_max_i8(m, s);
         g.part_sum[(size_t)tile_n * g.M + m0 + tid] = s;
     }
 }

@@ -322,3 +322,32 @@ def test_python_refusals():
                 dict(W_shards=[], W_scales=[], shard_offsets=[], logits_out=None), dict(local_max=good["local_sumexp"])):
         with pytest.raises(vp.VPError):
             vp.vp_output_fwd_i8_group(**{**good, **bad})
+
+
+@pytest.mark.parametrize("N,k", [(3, 128), (40, 256), (100, 2304), (300, 256), (300, 2304), (600, 2304)])
+@pytest.mark.parametrize("rows,nan", [([300, 1, 400], [300]), ([300, 400], list(range(300, 700))), ([300, 31], list(range(300, 331))),
+                                      ([600], list(range(128, 256))), ([600], list(range(256, 512))), ([600], list(range(512, 600))),
+                                      ([600], [599]), ([600], list(range(600))), ([33], [32]), ([129], [128]), ([257, 40], [256])])
+def test_sums_with_a_nan(rows, nan, N, k):
+    """A NaN makes the sums NaN that it is part of, also where a tile, a wavefront's part of one or a shard holds nothing else; the
+    other shards' statistics and, with a token's NaN, the other tokens' stay."""
+    import paper_2411_05288_amd as vp
+    clean, case, token = (Product(N, k, rows, "bf16", seed=8) for _ in range(3))
+    case.sW[nan] = np.nan
+    token.sH[N - 1] = np.nan
+    a, b, c = clean.run(), case.run(), token.run()
+    clean.check(a)
+    shard_of = np.repeat(np.arange(len(rows)), rows)
+    hit = sorted(set(shard_of[nan].tolist()))
+    rest = [r for r in range(len(rows)) if r not in hit]
+    for x, y in zip(a[:3], b[:3]):
+        assert torch.equal(x[rest], y[rest])
+    for x, y in zip(a[:3], c[:3]):
+        assert torch.equal(x[:, :-1], y[:, :-1])
+    assert bool(torch.isnan(b[1][hit]).all()) and bool(torch.isnan(c[1][:, -1]).all())
+    for stats, tokens in ((b, slice(None)), (c, slice(N - 1, N))):
+        m, s, loss = (torch.zeros(N, device="cuda") for _ in range(3))
+        vp.vp_combine_stats(*stats[:3], m, s, loss, torch.zeros(1, device="cuda"))
+        assert bool(torch.isnan(s[tokens]).all()) and bool(torch.isnan(loss[tokens]).all())
+        if stats is c:
+            assert bool(torch.isfinite(loss[:-1]).all())
