@@ -377,7 +377,7 @@ vp_status vp_grad_scale(const void* const* grads, const int64_t* counts, const i
  * The quotient is the exact one, so q does not depend on the order or width of any arithmetic.  A row of zeros has scale 0 and
  * q = 0; a row that holds an infinity or a NaN has scale NaN and q = 0 (its logits become NaN, other rows' do not).
  *   x [N,h] : in, type dt.   q [N, vp_i8_row_stride(h)] : out, int8, zero in the columns h and behind.   scales [N] : out, fp32, at
- *   any element.   No output shares memory with x or the other one.
+ *   any element (x and q are 16-byte aligned).   No output shares memory with x or the other one.
  * vp_i8_row_stride: h rounded up to a multiple of 128 (-1 for h < 1 or h > 130944: sums of products stay below 2^31).
  */
 int64_t vp_i8_row_stride(int64_t h);

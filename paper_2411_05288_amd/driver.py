@@ -362,10 +362,13 @@ def _on(stream):
 
 
 def quantize_rows(x: torch.Tensor, stream=None):
-    """The rows of x in 8-bit integers, and their scales: what OutputLayerI8Plan takes for a shard of the weights."""
+    """The rows of x in 8-bit integers, and their scales: what OutputLayerI8Plan takes for a shard of the weights.  (A shard cut from
+    a larger matrix begins at any element; the library takes matrices that begin at 16 bytes, so such a one is copied.)"""
     if x.dim() != 2:
         raise B.VPError("x must be [rows, h]")
     with _on(stream):
+        if x.is_contiguous() and x.data_ptr() % 16:
+            x = x.clone()
         q = torch.empty((x.shape[0], B.vp_i8_row_stride(x.shape[1])), dtype=torch.int8, device=x.device)
         scales = torch.empty((x.shape[0],), dtype=torch.float32, device=x.device)
     B.vp_quantize_rows(x, q, scales, stream)

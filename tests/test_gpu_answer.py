@@ -309,3 +309,18 @@ def test_tokens_follow_the_kept_logits(kind, change, model):
     behind = verify.tokens[1::2].cpu().numpy()[accepted == 1]
     assert within(np.bincount(behind, minlength=V), len(behind), p)
     assert (verify.tokens[1::2].cpu().numpy()[accepted == 0] == -1).all()
+
+
+@pytest.mark.parametrize("dtype,h", [(torch.float32, 101), (torch.bfloat16, 101), (torch.bfloat16, 130)])
+def test_rows_of_a_shard_cut_anywhere_become_integers(dtype, h):
+    """Shards that are views of a whole matrix, of uneven sizes: they begin at any element."""
+    import paper_2411_05288_amd as vp
+    W = (torch.randn(501, h, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda")).to(dtype)
+    q, scales = vp.quantize_rows(W)
+    stream = torch.cuda.Stream()
+    for at in (1, 2, 3, 7, 167, 334):
+        for argument in (None, stream):
+            stream.wait_stream(torch.cuda.current_stream())
+            a, b = vp.quantize_rows(W[at:], argument)
+            torch.cuda.current_stream().wait_stream(stream)
+            assert torch.equal(a, q[at:]) and torch.equal(b, scales[at:])
