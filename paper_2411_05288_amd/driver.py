@@ -21,6 +21,15 @@ import torch
 from . import binding as B
 
 
+def _on(stream):
+    """Context in which torch's own work runs on the same stream as the library's kernels."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream))
+    return torch.cuda.stream(stream)
+
+
 @dataclass
 class OutputLayerResult:
     loss: torch.Tensor            # [1] fp32
@@ -225,14 +234,6 @@ class OutputLayerPlan:
         if not self.grouped:
             self.workspace, self.A = buffers(nbytes, False)
 
-    def _on(self, stream):
-        """Context in which torch-side fills run on the same stream as the library's kernels."""
-        if stream is None:
-            return contextlib.nullcontext()
-        if not isinstance(stream, torch.cuda.Stream):
-            stream = torch.cuda.ExternalStream(int(stream))
-        return torch.cuda.stream(stream)
-
     # A view is made only of a shard with padding, and without a call per shard: on small workloads the host's work is what
     # bounds a step.
     def _real(self, tensors, r):
@@ -251,7 +252,7 @@ class OutputLayerPlan:
         for r in range(self.live if in_one_call else 0, self.p):
             v = self.valid[r]
             if v == 0:     # all padding: the neutral element of the combine (exp(-inf) = 0)
-                with self._on(stream):
+                with _on(stream):
                     self.local_max[r].fill_(float("-inf"))
                     self.local_sumexp[r].zero_()
                     self.local_target[r].zero_()
@@ -301,7 +302,7 @@ class OutputLayerPlan:
                                         dh_overwrite=first)
                     first = False
             if first:      # no shard holds a real vocabulary row (cannot happen: vocab_size > 0)
-                with self._on(stream):
+                with _on(stream):
                     self.dH.zero_()
 
     def backward(self, stream=None) -> None:
@@ -309,7 +310,7 @@ class OutputLayerPlan:
         for r in range(self.p):
             v = self.valid[r]
             if v < self.rows[r]:
-                with self._on(stream):
+                with _on(stream):
                     self.dW[r][v:].zero_()
             if v == 0 or self.grouped:
                 continue
@@ -333,7 +334,7 @@ class OutputLayerPlan:
         if self.clip_plan is None or not self.clip_plan.covers(grads):
             # the norm and the workspaces stay where they are as long as this plan lives: a captured call has their addresses
             need = B.vp_grad_workspace_bytes(len(grads))
-            with self._on(stream):      # (the memory of a stream: the current one's may be in use by work before this call)
+            with _on(stream):      # (the memory of a stream: the current one's may be in use by work before this call)
                 if self.clip_norm is None:
                     self.clip_norm = torch.empty((1,), dtype=torch.float32, device=self.dH.device)
                 if not self.clip_workspaces or self.clip_workspaces[-1].numel() < need:
@@ -350,15 +351,6 @@ class OutputLayerPlan:
         return OutputLayerResult(self.loss, self.loss_rows, self.global_max, self.global_sumexp,
                                  self.local_max, self.local_sumexp, self.local_target,
                                  self.dH, self.dW, self.logits)
-
-
-def _on(stream):
-    """Context in which torch's own work runs on the same stream as the library's kernels."""
-    if stream is None:
-        return contextlib.nullcontext()
-    if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(int(stream))
-    return torch.cuda.stream(stream)
 
 
 def quantize_rows(x: torch.Tensor, stream=None):
@@ -446,7 +438,7 @@ class KeptLogits:
         rows = [int(t.shape[1]) for t in self.logits]
         self.global_max, self.global_sumexp = (torch.empty((plan.N,), dtype=torch.float32, device=self.logits[0].device)
                                                for _ in range(2))
-        self.workspace = torch.empty((B.vp_logits_stats_workspace_bytes(plan.N, rows),), dtype=torch.uint8,
+        self.stats_workspace = torch.empty((B.vp_logits_stats_workspace_bytes(plan.N, rows),), dtype=torch.uint8,
                                      device=self.logits[0].device)
 
     def __getattr__(self, name):
@@ -455,7 +447,7 @@ class KeptLogits:
         return getattr(self.plan, name)
 
     def statistics(self, stream=None) -> None:
-        B.vp_logits_stats(self.logits, self.global_max, self.global_sumexp, self.workspace, stream)
+        B.vp_logits_stats(self.logits, self.global_max, self.global_sumexp, self.stats_workspace, stream)
 
 
 class DraftVerifyPlan:

@@ -138,7 +138,7 @@ def test_statistics_status_is_an_exception_and_the_call_is_not_made_again(librar
 
 class Kept:
     """What DraftVerifyPlan asks of a plan."""
-    N, valid, offsets, note = 3, [4, 0, 2], [0, 4, 8], "the plan's"
+    N, valid, offsets, workspace = 3, [4, 0, 2], [0, 4, 8], "the plan's"
 
     def __init__(self, logits=True):
         self.logits = [torch.zeros(3, 4), torch.zeros(3, 0), torch.zeros(3, 2)] if logits else None
@@ -165,7 +165,7 @@ def test_a_verification_takes_statistics_of_the_logits_it_reads(library, monkeyp
     for p in plans:
         assert p.global_max.data_ptr() not in call and p.global_sumexp.data_ptr() not in call
         assert p.global_max.tolist() == [1.0] * 3 and p.global_sumexp.tolist() == [2.0] * 3
-    assert verify.target.plan is plans[0] and verify.target.note == "the plan's" and verify.target.offsets == [0, 8]
+    assert verify.target.plan is plans[0] and verify.target.workspace == "the plan's" and verify.target.offsets == [0, 8]
     assert copy.copy(verify.target).plan is plans[0]
     with pytest.raises(AttributeError):
         verify.target.nothing
