@@ -389,7 +389,8 @@ vp_status vp_quantize_rows(const void* x, int64_t N, int64_t h, vp_dtype dt, int
  * and the statistics of Y as there.  k is the row stride of both matrices, a multiple of 128; columns that stand for nothing
  * are zero (in one of the two at least).  logits_out (with VP_SAVE_LOGITS) is of type logits_dt.  A temperature is a factor of
  * H_scales.
- *   H [N,k], W_shard [Vs,k] : in, int8.  H_scales [N], W_scales [Vs] : in, fp32, finite and not negative (a NaN makes its row or
+ *   H [N,k], W_shard [Vs,k] : in, int8.  H_scales [N], W_scales [Vs] : in, fp32, finite and not negative, W_scales also times
+ *   sums of the integers (a NaN makes its row or
  *   column of the logits NaN, and the sums of exponentials that these are part of; maxima are those of the other logits, and if
  *   there are none no number that stands for anything).  Everything else as for vp_output_fwd; vectors may start at any element.
  *   No output shares memory with an input or another output.

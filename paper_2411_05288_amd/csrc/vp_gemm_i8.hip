@@ -13,9 +13,9 @@ namespace {
 typedef unsigned uintx4u __attribute__((ext_vector_type(4), aligned(2)));
 
 // Few tokens: 32 TI of them and 32 WAVES vocabulary rows in a workgroup of WAVES wavefronts, which take 32 rows each.  W is read
-// once, so what counts is that enough of it is on its way: a ring of SLOTS k tiles of 128 integers, all but one of them in flight,
-// and as many workgroups on a compute unit as the LDS holds, so that one loads while another is at its ends.  A load instruction
-// takes 8 whole lines of 128 bytes (past the caches: W is not read again), 16 bytes per lane, straight into LDS.
+// once, so what counts is that enough of it is on its way: a ring of SLOTS k tiles of 128 integers, all but one of them in flight.
+// Up to 32 tokens two workgroups share a compute unit (80 KB of LDS each), so that one loads while the other is at its ends; beyond
+// that one has it to itself (96 KB up to 64 tokens, 144 up to 128).  A load instruction takes 8 whole lines of 128 bytes (past the caches: W is not read again), 16 bytes per lane, straight into LDS.
 //
 // A slot holds rows of 128 bytes, of W and then of H.  Chunk c of row r (16 bytes) sits at position c ^ (r / 2 % 8): 16
 // consecutive rows, which a read of LDS serves at a time, have the same chunk in 16 different groups of banks.
@@ -224,7 +224,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void gemm_i8_few_kernel(GemmI8Group 
 // Tiles of 128 tokens and 256 vocabulary rows, two workgroups on a compute unit, so that one multiplies while the other is at its
 // ends: where the sum is short, the statistics and stores of a tile take as long as its products.  A ring of three slots of 64
 // integers (A's 128 rows, then B's 256, 64 bytes each, laid out as in vp_gemm_bf16_fast.h), one multiplied while two are on their
-// way, one barrier per slot.
+// way, one barrier per slot.  Tiles go in rounds of two for each compute unit, the last of them as long as a full one: N=509 V=50001 in
+// 3 shards has 792 tiles for 512 places: 23 % of the places of two rounds stay empty.
 // Where it is taken: sums of up to PAIR_MOST_K integers.  The fast kernel -> this one, us: N=509 h=1001 V=50001 fp32 76 -> 57, N=1000
 // h=1536 V=50001 bf16 129 -> 111, N=4096 h=1024 V=32000 224 -> 182, h=2048 V=64000 647 -> 638, h=2560 V=64000 746 -> 791.
 // STREAM: outputs bypass the caches where there is more than one round of tiles, as in the fast kernel, but not fp32 rows that

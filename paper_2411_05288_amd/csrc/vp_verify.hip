@@ -8,9 +8,10 @@
 // one draw in 40.
 //
 // Small calls are bound by the chain of loads that leads to the row (one sequence of 4 drafts, V=32000: 6.3 us for the sums, 3.9 for
-// the search), large ones by fp64 instructions, 40 for a token's two weights (256 sequences of up to 8 drafts, V=256000 bf16: 92 us
-// for the sums, 0.76 of the vector units' time, 2.2 TB/s).  Loops one segment ahead, workgroups that are not all resident at once, a
-// launch of its own for the rows and exponentials of bf16 numbers from two tables in LDS (30 % fewer instructions) made no
+// the search), large ones by vector instructions, most of them fp64 and 40 for a token's two weights as the exponential is computed
+// here (256 sequences of up to 8 drafts, V=256000 bf16: 93 us for the sums, 2.2 TB/s; the vector units are busy for 0.68 of the
+// launch, and for 0.93 of the time that their compute unit has work).  Loops one segment ahead, workgroups that are not all resident
+// at once, a launch of its own for the rows and exponentials of bf16 numbers from two tables in LDS (30 % fewer instructions) made no
 // difference of more than 8 % there and cost the smaller calls as much.
 #include <climits>
 
