@@ -439,7 +439,7 @@ class KeptLogits:
         self.global_max, self.global_sumexp = (torch.empty((plan.N,), dtype=torch.float32, device=self.logits[0].device)
                                                for _ in range(2))
         self.stats_workspace = torch.empty((B.vp_logits_stats_workspace_bytes(plan.N, rows),), dtype=torch.uint8,
-                                     device=self.logits[0].device)
+                                           device=self.logits[0].device)
 
     def __getattr__(self, name):
         if name == "plan":      # (not made yet)
